@@ -384,6 +384,77 @@ strait_status strait_k_attention(void* stream, const void* qkv, const int32_t* v
 strait_status strait_k_argmax_f16(void* stream, const void* x, int32_t rows, int32_t n, int64_t row_stride,
                                   int32_t* top1, int32_t hp);
 
+/* ---- operators of a decoder that answers token by token: device pointers + stream ---------------
+ * Like the entry points above: asynchronous on `stream`, whose device must be the current one; nothing is allocated, so all of them may be
+ * captured into a graph.  Activations fp16.  What host arguments say is checked (E_INVALID, E_SHAPE); what lies in device memory (lengths, page
+ * numbers) is held inside the bounds that the host arguments give, as each entry says. */
+
+/* Rows of activations as 8-bit integers with one scale each: s = max |x| / 127, q = x * (1 / s) rounded to the nearest, ties to even (fp32; 0 where s
+ * is 0).  x [M] rows of K fp16, `pitch` elements from one to the next (a multiple of 8, >= K; columns of a wider tensor will do); q int8 [M][K]; scale fp32 [M].
+ * A row that holds an infinity or a NaN gets the scale NaN and codes of 0, so that a product with it is NaN.  K a multiple of 16 (E_SHAPE); x and q
+ * 16-byte aligned.  M = 0 does nothing. */
+strait_status strait_k_quantize_rows(void* stream, const void* x, int32_t M, int32_t K, int64_t pitch, int8_t* q, float* scale, int32_t hp);
+/* Y[M,N] = act(xs[m] ws[n] sum_k x[m,k] w[n,k] + bias[n] (+ res[m,n])): a product in 8-bit integers with a scale for each token (row of x int8 [M][K]) and
+ * each output channel (row of w int8 [N][K]).  The sum is exact (int32), the rest fp32, rounded once; bias fp32 [N] or NULL, res fp16 [M][N] or NULL,
+ * y fp16 [M][N] (fp32 when out_f32 != 0); y may be res.  K a multiple of 16 up to 131056 (E_SHAPE: beyond, 128 * 128 * K leaves int32); x and w 16-byte aligned, res and y by
+ * their element.  M = 0 does nothing.  All bits are the same whatever M a row is part of. */
+strait_status strait_k_gemm_i8(void* stream, const int8_t* x, const float* x_scale, const int8_t* w, const float* w_scale, const float* bias,
+                               int32_t M, int32_t N, int32_t K, int32_t act, const void* res, void* y, int32_t out_f32, int32_t hp);
+
+/* A paged cache of keys and values: k, v [pages][kv_heads][page_tokens][head_dim], 16-byte aligned.  STRAIT_KV_F16: fp16 (the scales are not
+ * looked at).  STRAIT_KV_I8: int8 codes, k_scale, v_scale fp32 [pages][kv_heads]; a code stands for code * scale of its page and head.
+ * page_tokens 32, 64, 128 or 256; head_dim 64 or 128 (E_SHAPE otherwise).  Neither has to be initialised. */
+typedef enum { STRAIT_KV_F16 = 0, STRAIT_KV_I8 = 1 } strait_kv_type;
+typedef struct strait_kv_cache {
+    void* k;
+    void* v;
+    float* k_scale;
+    float* v_scale;
+    int32_t type, pages, page_tokens, kv_heads, head_dim;
+} strait_kv_cache;
+/* What a step works on.  Sequence b brings the tokens q_start[b] .. q_start[b + 1] - 1 of the step's `tokens` (int32 [seqs + 1] on the device, never decreasing;
+ * none is allowed), and kv_len[b] (int32 [seqs]) tokens of it are in the cache, those of this step included: its i-th of n new tokens is at
+ * position p = kv_len[b] - n + i, which is row p % page_tokens of page page_table[b * table_pitch + p / page_tokens] (int32).
+ * max_q: at least the most tokens that a sequence brings; max_kv: at least the longest kv_len (host: they size the launches; 1 <= max_q <= tokens, ceil(max_kv /
+ * page_tokens) <= table_pitch, E_INVALID otherwise).  A sequence's tokens from the max_q-th on, and those outside every sequence, are left out: nothing is
+ * written for them.  A kv_len outside 0 .. max_kv counts as the nearer of the two.  Page numbers outside 0 .. pages - 1 are not followed.
+ * tokens = 0 does nothing. */
+typedef struct strait_kv_batch {
+    const int32_t* q_start;
+    const int32_t* kv_len;
+    const int32_t* page_table;
+    int32_t seqs, tokens, max_q, max_kv, table_pitch;
+} strait_kv_batch;
+
+/* The table that strait_k_kv_append rotates by, in host memory: table[p][j] = cos(p base^(-2j / dim)), table[p][dim / 2 + j] = sin(...) for
+ * j < dim / 2, angles and functions in 64 bits, rounded once.  dim even. */
+strait_status strait_rope_table(float* table, int32_t positions, int32_t dim, double base);
+/* A step's keys and values into the cache, with the rotation by their positions on the way; the queries are rotated with them.
+ * k, v: row t at t * pitch_k, t * pitch_v elements, [kv_heads][head_dim]; q: row t at t * pitch_q, [heads][head_dim], -> q_out [tokens][heads][head_dim] (q and q_out
+ * both NULL: no queries; q_out may be q where pitch_q = heads * head_dim).  Pitches multiples of 8, all tensors 16-byte aligned: the columns of a fused projection's output will do.
+ * rope: strait_rope_table's on the device, fp32 [rope_rows][rope_dim], rope_rows >= max_kv; or NULL (rope_dim 0): nothing is rotated.  rope_dim a multiple of 16 up to
+ * head_dim: the first rope_dim of each head are rotated, dimension j with j + rope_dim / 2, or 2j with 2j + 1 where `interleaved`:
+ *     (a, b) -> (a cos - b sin, b cos + a sin), each product and sum rounded to fp32.
+ * fp16 caches and q_out: rounded once.  int8 caches: with m the largest magnitude among a page's new tokens of one head, the page's scale becomes s' = max(s, m / 127), where
+ * s counts as 0 if the page's first token is among them; where s' > s the page's older codes c become c * (s / s') rounded; a new x becomes x * (1 / s')
+ * rounded (fp32, ties to even; 0 where s' is 0).  An infinity counts as 65504 and a NaN as 0 on their way into an int8 cache.
+ * Tokens at negative positions (kv_len smaller than the number of new tokens) are not stored, and their queries not rotated.  A page that is appended to must not
+ * appear twice among the batch's pages that are appended to. */
+strait_status strait_k_kv_append(void* stream, const strait_kv_cache* cache, const strait_kv_batch* batch, const void* q, const void* k, const void* v,
+                                 int64_t pitch_q, int64_t pitch_k, int64_t pitch_v, int32_t heads, const float* rope, int32_t rope_rows, int32_t rope_dim,
+                                 int32_t interleaved, void* q_out, int32_t hp);
+/* Attention of a step's tokens over the cache, which holds them already.  q fp16: row t at t * pitch_q, [heads][head_dim]; out fp16 [tokens][heads][head_dim]; heads a
+ * multiple of kv_heads, head h reads kv head h / (heads / kv_heads).  The token at position p sees key j where
+ *     j <= p  and  (window == 0  or  p - j < window  or  j < sinks),
+ * out = sum_j softmax_j(scale q . k_j) v_j over what it sees; a token that sees nothing (at a negative position) gets zeros.  Keys on pages that are not followed count as not seen,
+ * and pages of which no token of the step sees a key are not looked at (their numbers may be anything).  What lies in the cache behind a sequence's last token, or in keys that no
+ * token of its sequence's step sees, has no effect, be it infinite or NaN; an fp16 value that is infinite or NaN and that only some of a sequence's tokens see may reach the others through a
+ * probability of 0.  scale finite and > 0.  window, sinks >= 0.
+ * workspace: strait_k_attention_paged_workspace bytes (which may be 0), 16-byte aligned, used during the call only; calls that overlap need one each. */
+strait_status strait_k_attention_paged_workspace(const strait_kv_cache* cache, const strait_kv_batch* batch, int32_t heads, int32_t window, int32_t sinks, size_t* bytes);
+strait_status strait_k_attention_paged(void* stream, const strait_kv_cache* cache, const strait_kv_batch* batch, const void* q, int64_t pitch_q, int32_t heads,
+                                       float scale, int32_t window, int32_t sinks, void* out, void* workspace, size_t workspace_bytes, int32_t hp);
+
 /* ---- host-to-device link model (host only; no GPU needed) -----------------------------------
  * Section 3.2 of the paper, "Interference in data transfer": pinned transfers of concurrent
  * batches are served first-in first-out, so

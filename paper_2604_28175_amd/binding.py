@@ -111,6 +111,12 @@ _SIGS = {
     "strait_k_layernorm": (_i32, [_vp, _vp, _vp, _vp, _i32, _i32, C.c_float, _vp, _i32]),
     "strait_k_attention": (_i32, [_vp, _vp, _vp, _i32, _i32, _i32, _vp, _i32]),
     "strait_k_argmax_f16": (_i32, [_vp, _vp, _i32, _i32, _i64, _vp, _i32]),
+    "strait_k_quantize_rows": (_i32, [_vp, _vp, _i32, _i32, _i64, _vp, _vp, _i32]),
+    "strait_k_gemm_i8": (_i32, [_vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _vp, _vp, _i32, _i32]),
+    "strait_rope_table": (_i32, [_vp, _i32, _i32, _f64]),
+    "strait_k_kv_append": (_i32, [_vp, _vp, _vp, _vp, _vp, _vp, _i64, _i64, _i64, _i32, _vp, _i32, _i32, _i32, _vp, _i32]),
+    "strait_k_attention_paged_workspace": (_i32, [_vp, _vp, _i32, _i32, _i32, C.POINTER(_sz)]),
+    "strait_k_attention_paged": (_i32, [_vp, _vp, _vp, _vp, _i64, _i32, C.c_float, _i32, _i32, _vp, _vp, _sz, _i32]),
     "strait_link_create": (_i32, [C.POINTER(_vp)]),
     "strait_link_destroy": (_i32, [_vp]),
     "strait_link_available": (_i32, [_vp, C.POINTER(_i64)]),
@@ -565,6 +571,202 @@ def k_argmax_f16(x, n, row_stride, rows, hp=0, stream=None):
     top1 = torch.empty((rows,), dtype=torch.int32, device=x.device)
     _check(lib.strait_k_argmax_f16(_stream(stream), _dev(x), rows, n, row_stride, _dev(top1), hp))
     return top1
+
+
+# ---- operators of a decoder (device tensors, like the above; what does not fit is refused before anything is launched) ----
+
+KV_F16, KV_I8 = 0, 1
+
+
+class KvCacheDesc(C.Structure):
+    """strait_kv_cache."""
+    _fields_ = [("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp), ("type", _i32), ("pages", _i32), ("page_tokens", _i32),
+                ("kv_heads", _i32), ("head_dim", _i32)]
+
+
+class KvBatchDesc(C.Structure):
+    """strait_kv_batch."""
+    _fields_ = [("q_start", _vp), ("kv_len", _vp), ("page_table", _vp), ("seqs", _i32), ("tokens", _i32), ("max_q", _i32), ("max_kv", _i32),
+                ("table_pitch", _i32)]
+
+
+def _require(ok: bool, why: str):
+    if not ok:
+        raise StraitError(E_INVALID, why)
+
+
+def _operand(t, dtype, shape, what: str, device=None):
+    """A dense tensor of this type and shape on a GPU (on `device`, if given); None in a shape is any size."""
+    _require(torch.is_tensor(t), f"{what} must be a tensor")
+    _require(t.is_cuda and (device is None or t.device == device), f"{what} must be on the GPU, on the device of the other tensors")
+    _require(t.dtype == dtype, f"{what} must be {dtype}, is {t.dtype}")
+    _require(t.dim() == len(shape) and all(a is None or a == b for a, b in zip(shape, t.shape)), f"{what} has shape {tuple(t.shape)}, not {shape}")
+    _require(t.is_contiguous(), f"{what} must be contiguous")
+
+
+def _rows(t, width, what: str, device=None):
+    """fp16 rows [T][width], which may be columns of a wider tensor; returns the elements from one to the next."""
+    _require(torch.is_tensor(t) and t.is_cuda and (device is None or t.device == device), f"{what} must be on the GPU, on the device of the other tensors")
+    _require(t.dtype == torch.float16 and t.dim() == 2 and (width is None or t.shape[1] == width), f"{what} must be float16 [tokens][{width}], is {t.dtype} {tuple(t.shape)}")
+    _require(t.shape[1] <= 1 or t.stride(1) == 1, f"{what}: the elements of a row must be adjacent")
+    return t.stride(0) if t.shape[0] > 1 else (t.shape[1] + 7) // 8 * 8
+
+
+class _On:
+    """The stream of a call, with the tensors' device made the current one for it, and tensors made for it told of a stream that is not theirs."""
+
+    def __init__(self, device, stream):
+        self.device, self.stream, self.guard = device, stream, None
+
+    def __enter__(self):
+        if torch.cuda.current_device() != self.device.index:
+            self.guard = torch.cuda.device(self.device)
+            self.guard.__enter__()
+        if self.stream is not None:
+            _require(self.stream.device == self.device, "the stream must be on the device of the tensors")
+        self.handle = _stream(self.stream)
+        return self
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+    def made(self, *tensors):
+        if self.stream is not None:
+            for t in tensors:
+                t.record_stream(self.stream)
+
+
+def k_quantize_rows(x, hp=0, stream=None):
+    """strait_k_quantize_rows of x fp16 [M][K] (rows may lie further apart); returns (codes int8 [M][K], scale fp32 [M])."""
+    pitch = _rows(x, None, "x")
+    m, k = x.shape
+    with _On(x.device, stream) as on:
+        q = torch.empty((m, k), dtype=torch.int8, device=x.device)
+        scale = torch.empty((m,), dtype=torch.float32, device=x.device)
+        on.made(q, scale)
+        _check(lib.strait_k_quantize_rows(on.handle, _dev(x), m, k, pitch, _dev(q), _dev(scale), hp))
+    return q, scale
+
+
+def k_gemm_i8(x, x_scale, w, w_scale, bias=None, act=ACT_NONE, res=None, out_f32=False, hp=0, stream=None):
+    """strait_k_gemm_i8: x int8 [M][K] and its rows' scales, w int8 [N][K] and its rows' scales; returns y [M][N]."""
+    _operand(x, torch.int8, (None, None), "x")
+    m, k = x.shape
+    _operand(w, torch.int8, (None, k), "w", x.device)
+    n = w.shape[0]
+    _operand(x_scale, torch.float32, (m,), "x_scale", x.device)
+    _operand(w_scale, torch.float32, (n,), "w_scale", x.device)
+    if bias is not None:
+        _operand(bias, torch.float32, (n,), "bias", x.device)
+    if res is not None:
+        _operand(res, torch.float16, (m, n), "res", x.device)
+    with _On(x.device, stream) as on:
+        y = torch.empty((m, n), dtype=torch.float32 if out_f32 else torch.float16, device=x.device)
+        on.made(y)
+        _check(lib.strait_k_gemm_i8(on.handle, _dev(x), _dev(x_scale), _dev(w), _dev(w_scale), _dev(bias), m, n, k, act, _dev(res), _dev(y), int(out_f32), hp))
+    return y
+
+
+def rope_table(positions: int, dim: int, base: float = 10000.0) -> np.ndarray:
+    """strait_rope_table: fp32 [positions][dim] in host memory, cosines and then sines."""
+    t = np.empty((max(positions, 0), max(dim, 0)), dtype=np.float32)
+    _check(lib.strait_rope_table(_np_ptr(t), positions, dim, float(base)))
+    return t
+
+
+class KvCache:
+    """strait_kv_cache over the caller's tensors, which it keeps: k, v [pages][kv_heads][page_tokens][head_dim], fp16, or int8 with k_scale, v_scale fp32
+    [pages][kv_heads]."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        _require(torch.is_tensor(k) and k.dtype in (torch.float16, torch.int8), "k must be a float16 or int8 tensor")
+        _operand(k, k.dtype, (None,) * 4, "k")
+        _operand(v, k.dtype, tuple(k.shape), "v", k.device)
+        i8 = k.dtype == torch.int8
+        _require(i8 == (k_scale is not None) and i8 == (v_scale is not None), "an int8 cache has k_scale and v_scale, an fp16 cache none")
+        for t, what in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+            if i8:
+                _operand(t, torch.float32, tuple(k.shape[:2]), what, k.device)
+        self.k, self.v, self.k_scale, self.v_scale, self.device = k, v, k_scale, v_scale, k.device
+        self.pages, self.kv_heads, self.page_tokens, self.head_dim = k.shape
+        self.desc = KvCacheDesc(_dev(k), _dev(v), _dev(k_scale), _dev(v_scale), KV_I8 if i8 else KV_F16, self.pages, self.page_tokens, self.kv_heads, self.head_dim)
+        self.ref = C.byref(self.desc)
+
+
+class KvBatch:
+    """strait_kv_batch over the caller's int32 tensors, which it keeps and which may be rewritten between steps: q_start [seqs + 1], kv_len [seqs], page_table
+    [seqs][columns].  How many tokens a step has is the rows of the tensors that it is called with."""
+
+    def __init__(self, q_start, kv_len, page_table, max_q: int, max_kv: int):
+        _operand(kv_len, torch.int32, (None,), "kv_len")
+        _operand(q_start, torch.int32, (kv_len.shape[0] + 1,), "q_start", kv_len.device)
+        _operand(page_table, torch.int32, (kv_len.shape[0], None), "page_table", kv_len.device)
+        self.q_start, self.kv_len, self.page_table, self.device = q_start, kv_len, page_table, kv_len.device
+        self.desc = KvBatchDesc(_dev(q_start), _dev(kv_len), _dev(page_table), kv_len.shape[0], 0, max_q, max_kv, page_table.shape[1])
+        self._of = {}
+
+    def ref(self, tokens: int):
+        """strait_kv_batch of a step of so many tokens."""
+        r = self._of.get(tokens)
+        if r is None:
+            if len(self._of) > 256:
+                self._of.clear()
+            d = KvBatchDesc.from_buffer_copy(self.desc)
+            d.tokens = tokens
+            r = self._of[tokens] = C.byref(d)
+        return r
+
+
+def k_kv_append(cache: KvCache, batch: KvBatch, k, v, q=None, rope=None, interleaved=False, q_out=None, hp=0, stream=None):
+    """strait_k_kv_append of k, v fp16 [tokens][kv_heads * head_dim] (rows may lie further apart: columns of a fused projection's output); with q
+    [tokens][heads * head_dim], returns the rotated queries (in q_out, if given).  rope: rope_table() on the device."""
+    _require(cache.device == batch.device, "cache and batch must be on one device")
+    width = cache.kv_heads * cache.head_dim
+    pk, pv = _rows(k, width, "k", cache.device), _rows(v, width, "v", cache.device)
+    tokens = k.shape[0]
+    _require(v.shape[0] == tokens, "k and v have different numbers of tokens")
+    pq = heads = 0
+    if rope is not None:
+        _operand(rope, torch.float32, (None, None), "rope", cache.device)
+    _require(q is not None or q_out is None, "q_out without q")
+    with _On(cache.device, stream) as on:
+        if q is not None:
+            pq = _rows(q, None, "q", cache.device)
+            _require(q.shape[0] == tokens and q.shape[1] % cache.head_dim == 0, "q must be [tokens][heads * head_dim]")
+            heads = q.shape[1] // cache.head_dim
+            if q_out is None:
+                q_out = torch.empty((tokens, q.shape[1]), dtype=torch.float16, device=q.device)
+                on.made(q_out)
+            else:
+                _operand(q_out, torch.float16, tuple(q.shape), "q_out", cache.device)
+        _check(lib.strait_k_kv_append(on.handle, cache.ref, batch.ref(tokens), _dev(q), _dev(k), _dev(v), pq, pk, pv, heads, _dev(rope),
+                                      0 if rope is None else rope.shape[0], 0 if rope is None else rope.shape[1], int(interleaved), _dev(q_out), hp))
+    return q_out
+
+
+def k_attention_paged(q, cache: KvCache, batch: KvBatch, scale: float, window: int = 0, sinks: int = 0, out=None, hp=0, stream=None):
+    """strait_k_attention_paged of q fp16 [tokens][heads * head_dim] (rows may lie further apart); returns out, of the same shape (rows that belong to no
+    sequence are left as they are: of a tensor made here, undefined)."""
+    _require(cache.device == batch.device, "cache and batch must be on one device")
+    pitch = _rows(q, None, "q", cache.device)
+    tokens, width = q.shape
+    _require(width % cache.head_dim == 0, "q must be [tokens][heads * head_dim]")
+    heads = width // cache.head_dim
+    with _On(cache.device, stream) as on:
+        if out is None:
+            out = torch.empty((tokens, width), dtype=torch.float16, device=q.device)
+            on.made(out)
+        else:
+            _operand(out, torch.float16, (tokens, width), "out", cache.device)
+        need, ref = _sz(), batch.ref(tokens)
+        _check(lib.strait_k_attention_paged_workspace(cache.ref, ref, heads, window, sinks, C.byref(need)))
+        ws = None
+        if need.value:
+            ws = torch.empty((need.value,), dtype=torch.uint8, device=q.device)
+            on.made(ws)
+        _check(lib.strait_k_attention_paged(on.handle, cache.ref, ref, _dev(q), pitch, heads, scale, window, sinks, _dev(out), _dev(ws), need.value, hp))
+    return out
 
 
 class Link:

@@ -1,0 +1,610 @@
+"""A decoder's operators on the GPU against the oracle: products in 8-bit integers, appending to a paged cache, attention over it, and a run of them together.
+
+Tolerances.  fp16 results are off by half a step, 2^-11 of the value (2^-25 below the normal numbers), for their own rounding; what is added is said at each
+bound.  Codes of 8-bit integers and their scales are equal bit for bit: their definition names every operation.
+"""
+import numpy as np
+import pytest
+
+from oracle import decoder as D
+from oracle import ops
+
+pytestmark = pytest.mark.gpu
+HALF16, HALF32, TINY16 = 2.0 ** -11, 2.0 ** -24, 2.0 ** -25
+
+
+@pytest.fixture(scope="module")
+def S():
+    import torch
+    import paper_2604_28175_amd as strait
+    assert torch.cuda.is_available()
+    strait.torch = torch
+    return strait
+
+
+def dev(S, a):
+    return None if a is None else S.torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def host(t):
+    return t.cpu().numpy()
+
+
+def within(got, want, bound, what=""):
+    got, want = np.asarray(got, np.float64), np.asarray(want, np.float64)
+    assert got.shape == want.shape, (what, got.shape, want.shape)
+    off = np.abs(got - want) - bound
+    assert np.isfinite(got).all(), f"{what}: not finite"
+    assert (off <= 0).all(), f"{what}: {int((off > 0).sum())} of {off.size} off, worst {np.abs(got - want).max():.3e}, over its bound by {off.max():.3e}"
+
+
+def act_ref(y, act):
+    return {0: y, 1: ops.relu(y), 2: ops.relu6(y), 3: ops.gelu(y)}[act]
+
+
+# ---- products in 8-bit integers -------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("M,K", [(1, 16), (3, 48), (5, 2048), (9, 2064), (2, 8192), (3, 8208), (1, 20000), (260, 768)])
+def test_quantize_rows(S, M, K):
+    r = np.random.default_rng(M * 7 + K)
+    x = (r.standard_normal((M, K)) * np.exp(r.standard_normal((M, 1)) * 3)).astype(np.float16)
+    q, s = S.k_quantize_rows(dev(S, x))
+    want, scale = D.quantize_rows(x)
+    assert np.array_equal(host(s), scale) and np.array_equal(host(q), want)
+
+
+def test_quantize_rows_of_odd_contents_and_columns_of_a_wider_tensor(S):
+    r = np.random.default_rng(1)
+    x = r.standard_normal((12, 96)).astype(np.float16)
+    x[1] = 0                                                   # scale 0
+    x[2], x[3, 95], x[4, 0], x[5, 40] = 65504, np.inf, np.nan, -np.inf
+    x[6] = 0
+    x[6, 50] = 6e-8                                            # the smallest number
+    x[7] = -x[8]
+    wide = np.full((12, 160), np.nan, np.float16)
+    wide[:, 32:128] = x
+    q, s = S.k_quantize_rows(dev(S, wide)[:, 32:128])
+    want, scale = D.quantize_rows(x)
+    assert np.array_equal(host(s), scale, equal_nan=True) and np.array_equal(host(q), want)
+    assert np.isnan(host(s)[[3, 4, 5]]).all() and not host(q)[[1, 3, 4, 5]].any() and host(q)[6, 50] == 127
+    q, s = S.k_quantize_rows(dev(S, x)[:0])
+    assert q.shape == (0, 96) and s.shape == (0,)
+
+
+GEMM = [  # M, N, K, act, residual, fp32 out, bias
+    (1, 1, 16, 0, False, False, True), (1, 4096, 4096, 0, False, False, True), (1, 33, 131056, 0, False, True, False), (3, 70, 48, 3, True, False, True),
+    (5, 1000, 752, 1, False, False, True), (16, 100, 160, 0, True, False, True), (17, 33, 1024, 2, False, True, True), (31, 2304, 768, 0, False, False, True),
+    (32, 257, 2064, 0, True, True, True), (33, 257, 4096, 0, True, False, True), (64, 768, 4112, 3, False, False, True), (65, 128, 64, 0, False, False, False), (100, 5000, 512, 1, True, False, True),
+    (129, 300, 2064, 0, False, False, True), (200, 4096, 1024, 0, True, False, True), (257, 129, 80, 3, False, True, True), (300, 509, 528, 0, True, False, True),
+    (513, 1025, 1040, 0, True, False, True), (1000, 513, 272, 3, True, False, True), (2049, 770, 96, 0, False, False, True), (1500, 2500, 768, 0, True, True, True), (5000, 1024, 144, 1, False, False, True),
+]
+
+
+def product(S, r, M, N, K, act, use_res, out_f32, use_bias):
+    x, w = (r.integers(-128, 128, (n, K)).astype(np.int8) for n in (M, N))
+    # (scales of either size, so that outputs are of about 1)
+    xs, ws = (np.exp(r.standard_normal(n) * 0.5).astype(np.float32) * F for n, F in ((M, np.float32(3e-3)), (N, np.float32(6e-2 / K ** 0.5))))
+    bias = r.standard_normal(N).astype(np.float32) if use_bias else None
+    res = r.standard_normal((M, N)).astype(np.float16) if use_res else None
+    return x, xs, w, ws, bias, res
+
+
+def gemm_bound(x, xs, w, ws, bias, res, act, out_f32):
+    """The oracle's result, and how far off it may be: the sum is exact; its conversion, the product of the scales, the fused multiply-add and the residual's
+    addition round to fp32, each by at most half a step of what is there (4 |y| and the parts that cancel in it); no activation is steeper than 1.13; GELU's
+    own error is 2.4e-7; then the rounding of the result."""
+    z = D.gemm_i8(x, xs, w, ws)
+    y = D.gemm_i8(x, xs, w, ws, bias, res)
+    parts = np.abs(z) + (0 if bias is None else np.abs(bias)) + (0 if res is None else np.abs(res.astype(np.float64)))
+    want = act_ref(y, act)
+    return want, 1.13 * 5 * HALF32 * parts + (2.4e-7 if act == 3 else 0) + (HALF32 if out_f32 else HALF16) * np.abs(want) * 1.001 + (0 if out_f32 else TINY16)
+
+
+@pytest.mark.parametrize("case", GEMM, ids=lambda c: "x".join(map(str, c[:3])))
+def test_gemm_i8(S, case):
+    M, N, K, act, use_res, out_f32, use_bias = case
+    x, xs, w, ws, bias, res = product(S, np.random.default_rng(M + N + K), *case)
+    y = S.k_gemm_i8(dev(S, x), dev(S, xs), dev(S, w), dev(S, ws), dev(S, bias), act, dev(S, res), out_f32)
+    within(host(y), *gemm_bound(x, xs, w, ws, bias, res, act, out_f32), f"gemm_i8 {case}")
+
+
+def test_gemm_i8_rows_have_the_same_bits_in_every_batch(S):
+    r = np.random.default_rng(3)
+    x, xs, w, ws, bias, res = (dev(S, a) for a in product(S, r, 1300, 520, 784, 3, True, False, True))
+    whole = S.k_gemm_i8(x, xs, w, ws, bias, S.ACT_GELU, res)
+    for lo, hi in ((0, 1), (7, 12), (100, 116), (64, 100), (3, 70), (900, 1100), (0, 600)):
+        assert S.torch.equal(S.k_gemm_i8(x[lo:hi].contiguous(), xs[lo:hi].contiguous(), w, ws, bias, S.ACT_GELU, res[lo:hi].contiguous()), whole[lo:hi]), (lo, hi)
+
+
+def test_gemm_i8_largest_sums_and_scales_that_are_not_finite(S):
+    K = 131056
+    for M in (1, 40):
+        x, w = np.full((M, K), -128, np.int8), np.full((9, K), -128, np.int8)
+        w[1] = 127
+        one = np.ones
+        y = host(S.k_gemm_i8(dev(S, x), dev(S, one(M, np.float32)), dev(S, w), dev(S, one(9, np.float32)), out_f32=True))
+        assert (y == np.array([K * 128.0 * 128] + [K * -128.0 * 127] + [K * 128.0 * 128] * 7, np.float64).astype(np.float32)).all()
+    xs = one(M, np.float32)
+    xs[3] = np.nan
+    y = host(S.k_gemm_i8(dev(S, x), dev(S, xs), dev(S, w), dev(S, one(9, np.float32)), out_f32=True))
+    assert np.isnan(y[3]).all() and np.isfinite(np.delete(y, 3, 0)).all()
+
+
+def test_gemm_i8_into_its_residual(S):
+    """y may be res: a block's residual stream is updated where it lies."""
+    r = np.random.default_rng(4)
+    for M, N, K in ((3, 514, 512), (200, 514, 512)):
+        x, xs, w, ws, bias, res = (dev(S, a) for a in product(S, r, M, N, K, 0, True, False, True))
+        want = S.k_gemm_i8(x, xs, w, ws, bias, 0, res)
+        status = S.lib.strait_k_gemm_i8(S.torch.cuda.current_stream().cuda_stream, x.data_ptr(), xs.data_ptr(), w.data_ptr(), ws.data_ptr(), bias.data_ptr(), M, N, K, 0, res.data_ptr(), res.data_ptr(), 0, 0)
+        assert status == S.OK and S.torch.equal(res, want)
+
+
+# ---- a batch over a paged cache -----------------------------------------------------------------------------------------
+
+class World:
+    """A cache, its pages dealt to sequences in no order, and a step's batch."""
+
+    def __init__(self, S, seed, new, past, kv_heads, group, dim, page, i8, spare=2, fill=True):
+        r = self.r = np.random.default_rng(seed)
+        self.S, self.new, self.total = S, list(new), [a + b for a, b in zip(new, past)]
+        self.H, self.G, self.D, self.P, self.i8 = kv_heads, group, dim, page, i8
+        each = [-(-t // page) for t in self.total]
+        self.pages = sum(each) + spare
+        order = r.permutation(self.pages)
+        self.table = np.full((len(new), max(each + [1])), -1, np.int32)
+        for b, n in enumerate(each):
+            self.table[b, :n], order = order[:n], order[n:]
+        self.q_start = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+        self.kv_len = np.array(self.total, np.int32)
+        self.tokens = int(sum(new))
+        self.max_q, self.max_kv = max(1, max(new)), max(1, max(self.total))
+        shape = (self.pages, kv_heads, page, dim)
+        if i8:
+            self.k, self.v = (np.clip(np.rint(r.standard_normal(shape) * 36), -127, 127).astype(np.int8) for _ in range(2))
+            self.ks, self.vs = (np.exp(r.standard_normal(shape[:2]) * 0.3).astype(np.float32) * np.float32(0.03) for _ in range(2))
+        else:
+            self.k, self.v = (r.standard_normal(shape).astype(np.float16) for _ in range(2))
+            self.ks = self.vs = None
+
+    def where(self):
+        return list(D.places(self.q_start, self.kv_len, self.table, self.P, self.pages, self.max_q, self.max_kv, self.tokens))
+
+    def on_gpu(self):
+        S = self.S
+        self.cache = S.KvCache(dev(S, self.k), dev(S, self.v), dev(S, self.ks), dev(S, self.vs))
+        self.batch = S.KvBatch(dev(S, self.q_start), dev(S, self.kv_len), dev(S, self.table), self.max_q, self.max_kv)
+        return self
+
+    def taken_back(self):
+        """What the cache on the GPU holds."""
+        c = self.cache
+        return [None if t is None else host(t) for t in (c.k, c.v, c.k_scale, c.v_scale)]
+
+    def values(self):
+        k, v = (a.astype(np.float64) for a in (self.k, self.v))
+        return (k * self.ks.astype(np.float64)[..., None, None], v * self.vs.astype(np.float64)[..., None, None]) if self.i8 else (k, v)
+
+    def attention(self, q, scale, window=0, sinks=0):
+        """The oracle's output [tokens][heads * D], the bound of its error, and the rows that are written."""
+        k, v = self.values()
+        out, bound = np.zeros((self.tokens, self.H * self.G * self.D)), np.zeros((self.tokens, self.H * self.G * self.D))
+        rows = self.where()
+        for b in {w[0] for w in rows}:
+            mine = [(t, p) for s, t, p, _, _ in rows if s == b]
+            t, p = np.array([m[0] for m in mine]), np.array([m[1] for m in mine])
+            total = min(max(int(self.kv_len[b]), 0), self.max_kv)
+            pages = self.table[b, :-(-total // self.P)]
+            good = np.repeat((pages >= 0) & (pages < self.pages), self.P)[:total]
+            at = np.where((pages >= 0) & (pages < self.pages), pages, 0)
+            for h in range(self.H):
+                kk, vv = (a[at, h].reshape(-1, self.D)[:total] for a in (k, v))
+                for g in range(self.G):
+                    c = slice((h * self.G + g) * self.D, (h * self.G + g + 1) * self.D)
+                    qq = q[t, c].astype(np.float64)
+                    o, mag = D.attention(qq, kk, vv, p, scale, window, sinks, good)
+                    out[t, c] = o
+                    # Half a step of the output.  The probabilities are rounded to fp16 (half a step each, or 2^-25 of the largest one below the normal numbers), and so may be the
+                    # values (half a step).  A score is a sum of D products in fp32, multiplied, subtracted from and raised to a power of 2, each rounding half a step of fp32 of the sum of magnitudes.
+                    kmax = np.abs(np.where(np.isfinite(kk), kk, 0)).max(initial=0)
+                    score = (np.abs(qq).sum(1, keepdims=True) * kmax) * scale * (self.D + 8) * HALF32
+                    vmax = np.abs(np.where(np.isfinite(vv), vv, 0)).max(initial=0)
+                    bound[t, c] = HALF16 * 1.001 * np.abs(o) + (2 * HALF16 + 2 * score + 64 * HALF32) * mag + total * TINY16 * vmax + TINY16
+        return out, bound, sorted({w[1] for w in rows})
+
+
+def check_attention(S, w, window=0, sinks=0, q_scale=2.0, scale=None, stream=None):
+    scale = w.D ** -0.5 if scale is None else scale
+    q = (w.r.standard_normal((w.tokens, w.H * w.G * w.D)) * q_scale).astype(np.float16)
+    w.on_gpu()
+    out = S.torch.full((w.tokens, q.shape[1]), 7.0, dtype=S.torch.float16, device="cuda")
+    S.k_attention_paged(dev(S, q), w.cache, w.batch, scale, window, sinks, out=out)
+    want, bound, rows = w.attention(q, scale, window, sinks)
+    got = host(out)
+    within(got[rows], want[rows], bound[rows], "attention")
+    rest = np.setdiff1d(np.arange(w.tokens), rows)
+    assert (got[rest] == 7.0).all()
+    return got
+
+
+# ---- appending ----------------------------------------------------------------------------------------------------------
+
+APPEND = [  # new, past, kv heads, group, dim, page, rotated, interleaved
+    ([1], [0], 1, 1, 64, 32, 64, False),
+    ([1, 1, 1, 1, 1], [0, 31, 32, 100, 63], 2, 4, 128, 64, 128, False),
+    ([70, 1, 0, 33, 64], [0, 5, 9, 31, 64], 2, 2, 64, 32, 32, True),
+    ([300, 129], [0, 127], 3, 1, 128, 128, 48, False),
+    ([2, 257, 256, 1], [255, 0, 1, 511], 1, 3, 64, 256, 16, True),
+    ([5, 17], [60, 0], 2, 2, 128, 64, 0, False),
+    ([1] * 150, [i * 3 % 70 for i in range(150)], 1, 2, 64, 64, 64, True),
+]
+
+
+def append_inputs(w, rope_dim, seed=9):
+    r = np.random.default_rng(seed)
+    qkv = (r.standard_normal((w.tokens, (w.H * w.G + 2 * w.H) * w.D)) * np.exp(r.standard_normal((w.tokens, 1)))).astype(np.float16)
+    rope = w.S.rope_table(w.max_kv + 3, rope_dim) if rope_dim else None
+    a, b = w.H * w.G * w.D, w.H * (w.G + 1) * w.D
+    return qkv, qkv[:, :a], qkv[:, a:b], qkv[:, b:], rope
+
+
+def check_append(w, q, k, v, rope, interleaved, got_q, held):
+    where = w.where()
+    heads = lambda x: x.reshape(w.tokens, -1, w.D)
+    for x, codes, scale, got, got_scale, turn in ((k, w.k, w.ks, held[0], held[2], rope), (v, w.v, w.vs, held[1], held[3], None)):
+        if w.i8:
+            codes, scale = codes.copy(), scale.copy()
+            D.append_int8(codes, scale, heads(x), where, turn, interleaved)
+            assert np.array_equal(got_scale, scale, equal_nan=True) and np.array_equal(got, codes)
+        else:
+            want, bound = codes.astype(np.float64), np.zeros(codes.shape)
+            for _, t, p, g, row in where:
+                if p >= 0 and g >= 0:
+                    want[g, :, row] = D.rotate(heads(x)[t].astype(np.float64), p, 0 if turn is None else turn.shape[1], 10000.0, interleaved)
+                    # half a step, and in fp32 the table's and three operations' of two numbers of at most the head's largest
+                    bound[g, :, row] = HALF16 * 1.001 * np.abs(want[g, :, row]) + TINY16 + 8 * HALF32 * np.abs(heads(x)[t].astype(np.float64)).max(1, keepdims=True)
+            within(got, want, bound, "cache")
+    if q is not None:
+        done = {t: p for _, t, p, _, _ in where}
+        rows = sorted(done)
+        x = heads(q).astype(np.float64)
+        want = np.stack([D.rotate(x[t], done[t], 0 if rope is None or done[t] < 0 else rope.shape[1], 10000.0, interleaved).reshape(-1) for t in rows])
+        top = np.repeat(np.abs(x[rows]).max(2), w.D, 1)
+        within(got_q[rows], want, HALF16 * 1.001 * np.abs(want) + TINY16 + 8 * HALF32 * top, "queries")
+        return rows
+
+
+@pytest.mark.parametrize("i8", [False, True], ids=["fp16", "int8"])
+@pytest.mark.parametrize("case", APPEND, ids=lambda c: f"{len(c[0])}seqs-{max(c[0])}new-{c[4]}-{c[5]}-r{c[6]}")
+def test_kv_append(S, case, i8):
+    new, past, H, G, dim, page, rotated, interleaved = case
+    w = World(S, 11, new, past, H, G, dim, page, i8).on_gpu()
+    qkv, q, k, v, rope = append_inputs(w, rotated)
+    wide = dev(S, qkv)
+    a, b = q.shape[1], q.shape[1] + k.shape[1]
+    got = S.k_kv_append(w.cache, w.batch, wide[:, a:b], wide[:, b:], q=wide[:, :a], rope=dev(S, rope), interleaved=interleaved)
+    check_append(w, q, k, v, rope, interleaved, host(got), w.taken_back())
+
+
+@pytest.mark.parametrize("i8", [False, True], ids=["fp16", "int8"])
+def test_kv_append_leaves_out_what_belongs_nowhere(S, i8):
+    """Tokens behind the last sequence and before the first, beyond max_q, at negative positions, on pages outside the cache; lengths outside 0 .. max_kv."""
+    w = World(S, 12, [3, 4, 40, 2, 6], [0, 5, 30, 9, 70], 2, 2, 64, 32, i8)
+    w.q_start = w.q_start + 2                                    # two tokens in front
+    w.tokens += 5                                                # and three behind
+    w.kv_len[1], w.kv_len[3] = 2, -5                             # two of sequence 1's tokens at negative positions, all of sequence 3's
+    w.table[2, 1], w.table[4, 2] = -1, w.pages
+    w.max_q = 35
+    w.kv_len[4], w.max_kv = 1 << 30, 76
+    w.on_gpu()
+    qkv, q, k, v, rope = append_inputs(w, 64)
+    wide = dev(S, qkv)
+    a, b = q.shape[1], q.shape[1] + k.shape[1]
+    out = S.torch.full((w.tokens, a), 7.0, dtype=S.torch.float16, device="cuda")
+    got = S.k_kv_append(w.cache, w.batch, wide[:, a:b], wide[:, b:], q=wide[:, :a], rope=dev(S, rope), q_out=out)
+    assert got is out
+    rows = check_append(w, q, k, v, rope, False, host(got), w.taken_back())
+    rest = np.setdiff1d(np.arange(w.tokens), rows)
+    assert len(rest) == 5 + 5 and (host(got)[rest] == 7.0).all()
+
+
+def test_kv_append_in_place_without_queries_and_without_tokens(S):
+    for i8 in (False, True):
+        w = World(S, 13, [20, 3], [0, 40], 2, 2, 128, 32, i8).on_gpu()
+        qkv, q, k, v, rope = append_inputs(w, 128)
+        dq = dev(S, q)
+        assert S.k_kv_append(w.cache, w.batch, dev(S, k), dev(S, v), rope=dev(S, rope)) is None
+        check_append(w, None, k, v, rope, False, None, w.taken_back())
+        w.on_gpu()
+        assert S.k_kv_append(w.cache, w.batch, dev(S, k), dev(S, v), q=dq, rope=dev(S, rope), q_out=dq) is dq
+        check_append(w, q, k, v, rope, False, host(dq), w.taken_back())
+        w.on_gpu()
+        before = w.taken_back()
+        S.k_kv_append(w.cache, w.batch, dev(S, k)[:0], dev(S, v)[:0])
+        assert all(x is None or np.array_equal(x, y) for x, y in zip(before, w.taken_back()))
+
+
+def test_kv_append_int8_of_odd_numbers(S):
+    """Infinities count as 65504 and NaN as 0; pages of zeros have scale 0; a fresh page's old scale and codes may be anything; a scale that does not grow leaves old codes alone."""
+    w = World(S, 14, [4, 5, 3, 2], [0, 64, 7, 7], 2, 1, 64, 64, True)
+    first = w.table[0, 0], w.table[1, 1]
+    for g in first:
+        w.ks[g], w.vs[g] = np.nan, np.inf
+    w.ks[w.table[2, 0]] = w.vs[w.table[2, 0]] = 100.0
+    w.on_gpu()
+    qkv, q, k, v, rope = append_inputs(w, 64)
+    qkv[0, 70], qkv[1, 200], qkv[2, 131], qkv[3, 5] = np.inf, -np.inf, np.nan, np.nan
+    qkv[4:9] = 0
+    a, b = q.shape[1], q.shape[1] + k.shape[1]
+    k, v = qkv[:, a:b], qkv[:, b:]
+    S.k_kv_append(w.cache, w.batch, dev(S, k), dev(S, v), rope=dev(S, rope))
+    held = w.taken_back()
+    check_append(w, None, k, v, rope, False, None, held)
+    assert not held[2][first[1]].any() and np.isfinite(held[2][list(first)]).all()
+    assert np.array_equal(held[0][w.table[2, 0], :, :7], w.k[w.table[2, 0], :, :7])
+
+
+def test_kv_append_beyond_32_bits(S):
+    """Pages more than 4 GiB into the cache."""
+    torch = S.torch
+    pages, H, P, dim = 18000, 8, 256, 128
+    w = World(S, 15, [3, 30], [1, 250], H, 1, dim, P, True)
+    k8, v8 = (torch.empty((pages, H, P, dim), dtype=torch.int8, device="cuda") for _ in range(2))
+    ks, vs = (torch.ones((pages, H), device="cuda") for _ in range(2))
+    at = {int(g): pages - 1 - i * 3 for i, g in enumerate(sorted(set(w.table[w.table >= 0].tolist())))}
+    for g, far in at.items():
+        k8[far], v8[far], ks[far], vs[far] = dev(S, w.k[g]), dev(S, w.v[g]), dev(S, w.ks[g]), dev(S, w.vs[g])
+    table = np.vectorize(lambda g: at.get(int(g), -1))(w.table).astype(np.int32)
+    w.cache = S.KvCache(k8, v8, ks, vs)
+    w.batch = S.KvBatch(dev(S, w.q_start), dev(S, w.kv_len), dev(S, table), w.max_q, w.max_kv)
+    qkv, q, k, v, rope = append_inputs(w, 64)
+    S.k_kv_append(w.cache, w.batch, dev(S, k), dev(S, v), rope=dev(S, rope))
+    held = [a.copy() for a in (w.k, w.v, w.ks, w.vs)]
+    for g, far in at.items():
+        for mine, there in zip(held, (k8, v8, ks, vs)):
+            mine[g] = host(there[far])
+    check_append(w, None, k, v, rope, False, None, held)
+    x = (w.r.standard_normal((w.tokens, H * dim)) * 2).astype(np.float16)
+    w.k, w.v, w.ks, w.vs = held
+    want, bound, rows = w.attention(x, 0.09)
+    within(host(S.k_attention_paged(dev(S, x), w.cache, w.batch, 0.09))[rows], want[rows], bound[rows])
+
+
+# ---- attention ------------------------------------------------------------------------------------------------------------
+
+ATTEND = [  # new, past, kv heads, group, dim, page
+    ([1], [0], 1, 1, 64, 32),
+    ([1], [4100], 2, 4, 128, 64),
+    ([1, 1, 1], [31, 32, 1000], 2, 1, 128, 32),
+    ([1] * 20, [37 * i % 311 for i in range(20)], 1, 8, 64, 128),
+    ([3, 0, 1, 5], [10, 4, 0, 95], 2, 3, 64, 64),
+    ([2, 4], [700, 0], 1, 7, 128, 256),
+    ([1, 1], [600, 3], 1, 40, 128, 64),
+    ([1], [300], 1, 71, 64, 64),
+    ([9, 8], [0, 200], 2, 8, 128, 64),
+    ([130, 1, 64], [0, 77, 200], 2, 2, 64, 32),
+    ([257, 300], [0, 31], 1, 1, 128, 64),
+    ([70, 1, 1], [3000, 2500, 8], 1, 4, 128, 64),
+    ([513], [1000], 1, 3, 64, 128),
+]
+
+
+@pytest.mark.parametrize("i8", [False, True], ids=["fp16", "int8"])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (1, 0), (50, 3), (200, 70)])
+@pytest.mark.parametrize("case", ATTEND, ids=lambda c: f"{len(c[0])}seqs-{max(c[0])}new-{max(c[1])}past-{c[2]}x{c[3]}x{c[4]}-{c[5]}")
+def test_attention_paged(S, case, window, sinks, i8):
+    new, past, H, G, dim, page = case
+    check_attention(S, World(S, 21, new, past, H, G, dim, page, i8), window, sinks)
+
+
+@pytest.mark.parametrize("i8", [False, True], ids=["fp16", "int8"])
+@pytest.mark.parametrize("new,max_q", [([3, 4, 2, 6], 5), ([3, 140, 2, 6], 120)], ids=["few", "many"])
+def test_attention_paged_where_nothing_is_to_be_seen(S, i8, new, max_q):
+    """Negative positions and empty caches give zeros; keys on pages that are not followed are not seen; tokens outside every sequence are left as they were."""
+    w = World(S, 22, new, [0, 5, 30, 90], 2, 2, 64, 32, i8)
+    w.q_start = w.q_start + 2
+    w.tokens += 5
+    w.kv_len[0], w.kv_len[2] = 1, -3
+    w.table[1, 0], w.table[3, 1] = -1, w.pages
+    w.max_q = max_q
+    got = check_attention(S, w)
+    assert not got[2:4].any() and got[4].any()
+
+
+@pytest.mark.parametrize("i8", [False, True], ids=["fp16", "int8"])
+@pytest.mark.parametrize("new,past", [([1, 1], [70, 200]), ([40, 1], [70, 200]), ([1], [3000])])
+def test_attention_paged_what_nobody_sees_may_be_anything(S, i8, new, past):
+    """NaN behind a sequence's last token and in front of every window, infinite scales and wild numbers of pages that no window reaches."""
+    window, sinks = 40, 3
+    w = World(S, 23, new, past, 2, 2, 128, 64, i8)
+    for b, t in enumerate(w.total):
+        g = w.table[b, (t - 1) // 64]
+        if not i8:
+            for a in (w.k, w.v):
+                a[g, :, (t - 1) % 64 + 1:] = np.nan
+                for j in range(3, t - w.new[b] - window + 1):
+                    a[w.table[b, j // 64], :, j % 64] = np.inf
+        for c in range(1, (t - w.new[b] - window + 1) // 64):
+            w.table[b, c] = (1 << 30) if c % 2 else -7
+    unused = np.setdiff1d(np.arange(w.pages), w.table)
+    if i8:
+        w.ks[unused], w.vs[unused] = np.nan, np.inf
+    else:
+        w.k[unused], w.v[unused] = np.nan, np.nan
+    check_attention(S, w, window, sinks)
+
+
+@pytest.mark.parametrize("i8", [False, True], ids=["fp16", "int8"])
+@pytest.mark.parametrize("new,past", [([1], [900]), ([150], [100])])
+def test_attention_paged_extreme_scores(S, i8, new, past):
+    """Scores of hundreds, one key that takes all, keys in rising order (the running maximum moves with every block), a page of much larger values."""
+    w = World(S, 24, new, past, 1, 4, 64, 32, i8)
+    check_attention(S, w, q_scale=60.0)
+    for j in range(w.total[0]):
+        g, row = w.table[0, j // 32], j % 32
+        w.k[g, :, row] = 100 if i8 else np.float16(3.0)
+        if i8:
+            w.ks[g] = np.float32(0.02 + 0.0005 * (j // 32))
+        else:
+            w.k[g, :, row] = np.float16(2.0 + 0.001 * j)
+    q = np.abs(w.r.standard_normal((w.tokens, 4 * 64))).astype(np.float16) * np.float16(2)
+    w.on_gpu()
+    want, bound, rows = w.attention(q, 0.5)
+    within(host(S.k_attention_paged(dev(S, q), w.cache, w.batch, 0.5)), want, bound)
+    w = World(S, 25, new, past, 1, 4, 64, 32, i8)
+    g = w.table[0, 1]
+    if i8:
+        w.vs[g] *= 1000
+        w.ks[w.table[0, 2]] *= 50
+    else:
+        w.v[g] *= np.float16(500)
+        w.k[w.table[0, 2]] *= np.float16(20)
+    check_attention(S, w)
+
+
+def test_attention_paged_shared_pages_and_strided_queries(S):
+    """Two sequences that read the same prompt's pages, and queries that are columns of a wider tensor; another scale."""
+    for i8 in (False, True):
+        w = World(S, 26, [1, 2], [128, 129], 2, 2, 64, 64, i8)
+        w.table[1, :2] = w.table[0, :2]
+        w.on_gpu()
+        wide = (w.r.standard_normal((w.tokens, 512)) * 2).astype(np.float16)
+        want, bound, _ = w.attention(wide[:, 128:384], 0.3)
+        within(host(S.k_attention_paged(dev(S, wide)[:, 128:384], w.cache, w.batch, 0.3)), want, bound)
+
+
+def test_the_binding_refuses_tensors_that_do_not_fit(S):
+    torch = S.torch
+    w = World(S, 27, [2], [30], 2, 2, 64, 32, True).on_gpu()
+    half = lambda *s: torch.zeros(s, dtype=torch.float16, device="cuda")
+    c = w.cache
+    bad = [lambda: S.k_quantize_rows(half(4, 64).t()), lambda: S.k_quantize_rows(half(4, 64).float()), lambda: S.k_quantize_rows(half(4, 72)[:, 4:68]),
+           lambda: S.KvCache(c.k, c.v), lambda: S.KvCache(c.k, c.v[:1], c.k_scale, c.v_scale), lambda: S.KvCache(c.k, c.v, c.k_scale, c.v_scale.half()),
+           lambda: S.KvCache(c.k.transpose(1, 2), c.v.transpose(1, 2), c.k_scale, c.v_scale), lambda: S.KvBatch(w.batch.q_start, w.batch.kv_len.long(), w.batch.page_table, 1, 1),
+           lambda: S.KvBatch(w.batch.kv_len, w.batch.kv_len, w.batch.page_table, 1, 1), lambda: S.k_attention_paged(half(2, 250), c, w.batch, 1.0),
+           lambda: S.k_attention_paged(half(2, 192), c, w.batch, 1.0), lambda: S.k_attention_paged(half(2, 256), c, w.batch, 1.0, out=half(2, 128)),
+           lambda: S.k_attention_paged(half(1, 256), c, w.batch, 1.0), lambda: S.k_kv_append(c, w.batch, half(2, 128), half(3, 128)), lambda: S.k_kv_append(c, w.batch, half(2, 64), half(2, 64)),
+           lambda: S.k_kv_append(c, w.batch, half(2, 128), half(2, 128), rope=half(40, 64)), lambda: S.k_kv_append(c, w.batch, half(2, 128), half(2, 128), q_out=half(2, 128)),
+           lambda: S.k_kv_append(c, w.batch, half(2, 128), half(2, 128), rope=half(10, 64).float())]
+    for i, call in enumerate(bad):
+        with pytest.raises(S.StraitError) as e:
+            call()
+        assert e.value.status == S.E_INVALID, i
+
+
+# ---- together -------------------------------------------------------------------------------------------------------------
+
+class Block:
+    """The attention half of a decoder's block in 8 bits: y = x + W_o attention(rotate(W_qkv x)), over a paged cache."""
+
+    def __init__(self, S, seed, H, G, dim, i8, window, sinks, lengths, page=32):
+        r = np.random.default_rng(seed)
+        self.S, self.H, self.G, self.dim, self.window, self.sinks = S, H, G, dim, window, sinks
+        self.width = H * G * dim
+        self.w = [D.quantize_rows((r.standard_normal((n, self.width)) * self.width ** -0.5).astype(np.float16)) for n in ((H * G + 2 * H) * dim, self.width)]
+        self.w = [tuple(dev(S, a) for a in w) for w in self.w]
+        self.world = World(S, seed, lengths, [0] * len(lengths), H, G, dim, page, i8).on_gpu()
+        self.rope = dev(S, S.rope_table(max(lengths), dim))
+
+    def step(self, x, batch, stream=None):
+        S = self.S
+        (wq, sq), (wo, so) = self.w
+        qkv = S.k_gemm_i8(*S.k_quantize_rows(x, stream=stream), wq, sq, stream=stream)
+        a, b = self.width, self.width + self.H * self.dim
+        q = S.k_kv_append(self.world.cache, batch, qkv[:, a:b], qkv[:, b:], q=qkv[:, :a], rope=self.rope, stream=stream)
+        o = S.k_attention_paged(q, self.world.cache, batch, self.dim ** -0.5, self.window, self.sinks, stream=stream)
+        return S.k_gemm_i8(*S.k_quantize_rows(o, stream=stream), wo, so, res=x, stream=stream)
+
+    def batch(self, new, total):
+        S, w = self.S, self.world
+        return S.KvBatch(dev(S, np.concatenate([[0], np.cumsum(new)]).astype(np.int32)), dev(S, np.array(total, np.int32)), w.batch.page_table, max(new), max(total))
+
+
+@pytest.mark.parametrize("i8,window,sinks", [(False, 0, 0), (True, 0, 0), (True, 24, 2)])
+def test_a_block_step_by_step(S, i8, window, sinks):
+    """Prompts of two sequences, then single tokens, some of them in the same step as another prompt's chunk; each operator against the oracle on what the one in front of it gave,
+    and the cache kept by the oracle through all steps."""
+    H, G, dim, lengths = 2, 2, 64, [75, 40, 66]
+    block = Block(S, 31, H, G, dim, i8, window, sinks, lengths)
+    w, r = block.world, np.random.default_rng(32)
+    done = [0, 0, 0]
+    for new in ([60, 33, 0], [1, 1, 0], [1, 1, 50], [1, 1, 1], [9, 0, 15], [1, 1, 0], [2, 3, 0]):
+        done = [a + b for a, b in zip(done, new)]
+        x = dev(S, r.standard_normal((sum(new), block.width)).astype(np.float16))
+        batch = block.batch(new, done)
+        (wq, sq), (wo, so) = block.w
+        codes, scale = S.k_quantize_rows(x)
+        qkv = S.k_gemm_i8(codes, scale, wq, sq)
+        within(host(qkv), *gemm_bound(host(codes), host(scale), host(wq), host(sq), None, None, 0, False), "qkv")
+        a, b = block.width, block.width + H * dim
+        q = S.k_kv_append(w.cache, batch, qkv[:, a:b], qkv[:, b:], q=qkv[:, :a], rope=block.rope)
+        w.q_start, w.kv_len, w.new, w.total = np.concatenate([[0], np.cumsum(new)]), np.array(done), new, done
+        w.tokens, w.max_q, w.max_kv = sum(new), max(new), max(done)
+        held = w.taken_back()
+        hqkv = host(qkv)
+        check_append(w, hqkv[:, :a], hqkv[:, a:b], hqkv[:, b:], host(block.rope), False, host(q), held)
+        w.k, w.v, w.ks, w.vs = held
+        o = S.k_attention_paged(q, w.cache, batch, dim ** -0.5, window, sinks)
+        want, bound, rows = w.attention(host(q), dim ** -0.5, window, sinks)
+        within(host(o)[rows], want[rows], bound[rows], "attention")
+        codes, scale = S.k_quantize_rows(o)
+        y = S.k_gemm_i8(codes, scale, wo, so, res=x)
+        within(host(y), *gemm_bound(host(codes), host(scale), host(wo), host(so), None, host(x), 0, False), "output")
+
+
+def test_a_block_on_another_stream_and_replayed_from_a_graph(S):
+    """The same bits: eagerly, on a stream that is not the current one, and from a captured graph whose inputs, lengths and pages are rewritten between replays."""
+    torch = S.torch
+    lengths = [500, 90, 40]
+    for i8 in (False, True):
+        blocks = [Block(S, 33, 2, 4, 128, i8, 0, 0, lengths) for _ in range(3)]
+        r = np.random.default_rng(34)
+        start = [300, 80, 33]
+        prompts = dev(S, r.standard_normal((sum(start), blocks[0].width)).astype(np.float16))
+        for b in blocks:
+            b.step(prompts, b.batch(start, start))
+        x = torch.zeros((3, blocks[0].width), dtype=torch.float16, device="cuda")
+        length = dev(S, np.array([301, 81, 34], np.int32))
+        ones = dev(S, np.arange(4).astype(np.int32))
+        # (lengths grow in place: the launches are made for the longest)
+        batches = [S.KvBatch(ones, length, b.world.batch.page_table, 1, 500) for b in blocks]
+        side = torch.cuda.Stream()
+        graph = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph):
+            y2 = blocks[2].step(x, batches[2])
+        for step in range(6):
+            x.copy_(dev(S, r.standard_normal((3, blocks[0].width)).astype(np.float16)))
+            y0 = blocks[0].step(x, batches[0])
+            side.wait_stream(torch.cuda.current_stream())
+            y1 = blocks[1].step(x, batches[1], stream=side)
+            torch.cuda.current_stream().wait_stream(side)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(y0, y1) and torch.equal(y0, y2), step
+            for a, b, c in zip(*(bl.world.taken_back() for bl in blocks)):
+                assert a is None or np.array_equal(a, b) and np.array_equal(a, c)
+            length += 1
+
+
+def test_chunks_give_what_a_whole_prompt_gives(S):
+    """An fp16 cache holds the same bits however its tokens came, and attention in chunks agrees with attention at once."""
+    w = World(S, 35, [333], [0], 2, 2, 64, 32, False)
+    r = np.random.default_rng(36)
+    q, k, v = ((r.standard_normal((333, n * 64)) * 2).astype(np.float16) for n in (4, 2, 2))
+    rope = dev(S, S.rope_table(333, 64))
+    w.on_gpu()
+    turned = S.k_kv_append(w.cache, w.batch, dev(S, k), dev(S, v), q=dev(S, q), rope=rope)
+    whole = host(S.k_attention_paged(turned, w.cache, w.batch, 0.125)).astype(np.float64)
+    held = w.taken_back()
+    w.on_gpu()
+    outs, at = [], 0
+    for n in (1, 100, 31, 1, 1, 150, 49):
+        batch = S.KvBatch(dev(S, np.array([0, n], np.int32)), dev(S, np.array([at + n], np.int32)), w.batch.page_table, n, at + n)
+        part = S.k_kv_append(w.cache, batch, dev(S, k[at:at + n]), dev(S, v[at:at + n]), q=dev(S, q[at:at + n]), rope=rope)
+        outs.append(host(S.k_attention_paged(part, w.cache, batch, 0.125)))
+        at += n
+    assert all(a is None or np.array_equal(a, b) for a, b in zip(held, w.taken_back()))
+    w.k, w.v = held[:2]
+    _, bound, _ = w.attention(host(turned), 0.125)
+    within(np.concatenate(outs), whole, 2 * bound)
