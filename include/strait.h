@@ -389,7 +389,7 @@ strait_status strait_k_argmax_f16(void* stream, const void* x, int32_t rows, int
  * captured into a graph.  Activations fp16.  What host arguments say is checked (E_INVALID, E_SHAPE); what lies in device memory (lengths, page
  * numbers) is held inside the bounds that the host arguments give, as each entry says. */
 
-/* Rows of activations as 8-bit integers with one scale each: s = max |x| / 127, q = x * (1 / s) rounded to the nearest, ties to even (fp32; 0 where s
+/* Rows of activations as 8-bit integers with one scale each: s = max |x| * (1 / 127), q = x * (1 / s) rounded to the nearest, ties to even (all in fp32; 0 where s
  * is 0).  x [M] rows of K fp16, `pitch` elements from one to the next (a multiple of 8, >= K; columns of a wider tensor will do); q int8 [M][K]; scale fp32 [M].
  * A row that holds an infinity or a NaN gets the scale NaN and codes of 0, so that a product with it is NaN.  K a multiple of 16 (E_SHAPE); x and q
  * 16-byte aligned.  M = 0 does nothing. */
@@ -435,7 +435,7 @@ strait_status strait_rope_table(float* table, int32_t positions, int32_t dim, do
  * rope: strait_rope_table's on the device, fp32 [rope_rows][rope_dim], rope_rows >= max_kv; or NULL (rope_dim 0): nothing is rotated.  rope_dim a multiple of 16 up to
  * head_dim: the first rope_dim of each head are rotated, dimension j with j + rope_dim / 2, or 2j with 2j + 1 where `interleaved`:
  *     (a, b) -> (a cos - b sin, b cos + a sin), each product and sum rounded to fp32.
- * fp16 caches and q_out: rounded once.  int8 caches: with m the largest magnitude among a page's new tokens of one head, the page's scale becomes s' = max(s, m / 127), where
+ * fp16 caches and q_out: rounded once.  int8 caches: with m the largest magnitude among a page's new tokens of one head, the page's scale becomes s' = max(s, m * (1 / 127)), where
  * s counts as 0 if the page's first token is among them; where s' > s the page's older codes c become c * (s / s') rounded; a new x becomes x * (1 / s')
  * rounded (fp32, ties to even; 0 where s' is 0).  An infinity counts as 65504 and a NaN as 0 on their way into an int8 cache.
  * Tokens at negative positions (kv_len smaller than the number of new tokens) are not stored, and their queries not rotated.  A page that is appended to must not

@@ -7,9 +7,9 @@ F = np.float32
 
 
 def quantize_rows(x):
-    """x fp16 [M][K] -> codes int8, scales fp32: s = max|x| / 127, q = rint(x * (1 / s)), all in fp32; a row that is not finite: NaN and zeros."""
+    """x fp16 [M][K] -> codes int8, scales fp32: s = max|x| * (1 / 127), q = rint(x * (1 / s)), all in fp32; a row that is not finite: NaN and zeros."""
     x = np.asarray(x).astype(F)
-    s = np.abs(x).max(1) / F(127)
+    s = np.abs(x).max(1) * (F(1) / F(127))
     fine = np.isfinite(s)
     with np.errstate(divide="ignore", invalid="ignore"):
         inv = np.where(fine & (s > 0), F(1) / s, F(0)).astype(F)
@@ -74,7 +74,7 @@ def append_int8(codes, scale, x, where, rope, interleaved):
         first = min(r for r, _ in rows)
         top = np.max([np.abs(y).max(1) for _, y in rows], 0).astype(F)
         before = scale[g] if first else np.zeros_like(top)
-        now = np.maximum(before, top / F(127)).astype(F)
+        now = np.maximum(before, top * (F(1) / F(127))).astype(F)
         for h in range(len(now)):
             if first and now[h] > before[h]:
                 codes[g, h, :first] = np.rint(codes[g, h, :first].astype(F) * (before[h] / now[h])).astype(np.int8)

@@ -118,7 +118,7 @@ __global__ void __launch_bounds__(256) kv_append_kernel(const KvAppend p, int pa
 #pragma unroll
         for (int i = 32; i; i >>= 1) top = __builtin_fmaxf(top, __shfl_xor(top, i));
         const bool fresh = lo == column * P;
-        const float before = fresh ? 0.f : *scale, candidate = top / 127.f, now = candidate > before ? candidate : before;
+        const float before = fresh ? 0.f : *scale, candidate = top * (1.f / 127.f), now = candidate > before ? candidate : before;
         if (!fresh && now > before) {
             const float by = before / now;
             for (int t = column * P + sub; t < lo; t += rows) {

@@ -1,6 +1,6 @@
 // Rows of activations as 8-bit integers with a scale each, the left operand of gemm_i8.hip, for gfx950.
 //
-//   s = max_k |x_k| / 127,   q_k = rint(x_k (1 / s))
+//   s = max_k |x_k| (1 / 127),   q_k = rint(x_k (1 / s))
 //
 // A row is read once and stays in registers between its maximum and its codes where it has at most 32 numbers per thread; 2 + 1 bytes per number, so
 // the memory bounds it.  A wavefront per row up to 2048 numbers (no barrier), four of them beyond.
@@ -49,7 +49,7 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const half_t* __rest
         for (int i = 0; i < 4; ++i) a = part[i] > a ? part[i] : a;
     }
     const bool finite = a < 0x7c00;
-    const float s = (float)__builtin_bit_cast(half_t, (unsigned short)a) / 127.f;
+    const float s = (float)__builtin_bit_cast(half_t, (unsigned short)a) * (1.f / 127.f);
     const float inv = finite && a ? 1.f / s : 0.f;
     if (t == 0) scale[m] = finite ? s : __builtin_nanf("");
     auto store = [&](int c, half8 v) __attribute__((always_inline)) {
