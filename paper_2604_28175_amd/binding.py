@@ -6,6 +6,7 @@ library is missing, importing this module raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 from typing import Optional, Sequence
@@ -590,81 +591,81 @@ class KvBatchDesc(C.Structure):
                 ("table_pitch", _i32)]
 
 
-def _require(ok: bool, why: str):
-    if not ok:
-        raise StraitError(E_INVALID, why)
+def _refuse(why: str):
+    raise StraitError(E_INVALID, why)
 
 
-def _operand(t, dtype, shape, what: str, device=None):
-    """A dense tensor of this type and shape on a GPU (on `device`, if given); None in a shape is any size."""
-    _require(torch.is_tensor(t), f"{what} must be a tensor")
-    _require(t.is_cuda and (device is None or t.device == device), f"{what} must be on the GPU, on the device of the other tensors")
-    _require(t.dtype == dtype, f"{what} must be {dtype}, is {t.dtype}")
-    _require(t.dim() == len(shape) and all(a is None or a == b for a, b in zip(shape, t.shape)), f"{what} has shape {tuple(t.shape)}, not {shape}")
-    _require(t.is_contiguous(), f"{what} must be contiguous")
+# (A step of single tokens is a few launches of a few microseconds each: what a call checks is checked in the cheapest order, and what is wrong is looked for only
+# where something is.)
+def _dense(t, dtype, shape, device: int, what: str):
+    """Refuses what is not a dense tensor of this type and shape (None: any size) on this GPU (-1: on any)."""
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and (t.shape == shape or len(shape) == t.dim() and all(a is None or a == b for a, b in zip(shape, t.shape)))
+            and t.is_contiguous() and t.is_cuda and (device < 0 or t.get_device() == device)):
+        _refuse(f"{what} must be a contiguous {dtype} tensor of shape {shape} on the GPU of the other tensors, is " +
+                (f"{t.dtype} {tuple(t.shape)} on {t.device}" if isinstance(t, torch.Tensor) else repr(type(t))))
 
 
-def _rows(t, width, what: str, device=None):
-    """fp16 rows [T][width], which may be columns of a wider tensor; returns the elements from one to the next."""
-    _require(torch.is_tensor(t) and t.is_cuda and (device is None or t.device == device), f"{what} must be on the GPU, on the device of the other tensors")
-    _require(t.dtype == torch.float16 and t.dim() == 2 and (width is None or t.shape[1] == width), f"{what} must be float16 [tokens][{width}], is {t.dtype} {tuple(t.shape)}")
-    _require(t.shape[1] <= 1 or t.stride(1) == 1, f"{what}: the elements of a row must be adjacent")
-    return t.stride(0) if t.shape[0] > 1 else (t.shape[1] + 7) // 8 * 8
+def _rows(t, width, device: int, what: str) -> int:
+    """fp16 rows [T][width] (None: any width), which may be columns of a wider tensor; the elements from one to the next."""
+    if not (isinstance(t, torch.Tensor) and t.dtype is torch.float16 and t.dim() == 2 and (width is None or t.size(1) == width) and t.is_cuda and
+            (device < 0 or t.get_device() == device) and (t.stride(1) == 1 or t.size(1) <= 1)):
+        _refuse(f"{what} must be float16 rows [tokens][{'width' if width is None else width}] of adjacent elements on the GPU of the other tensors, is " +
+                (f"{t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}" if isinstance(t, torch.Tensor) else repr(type(t))))
+    return t.stride(0) if t.size(0) > 1 else (t.size(1) + 7) // 8 * 8
 
 
-class _On:
-    """The stream of a call, with the tensors' device made the current one for it, and tensors made for it told of a stream that is not theirs."""
+_HERE = contextlib.nullcontext()
 
-    def __init__(self, device, stream):
-        self.device, self.stream, self.guard = device, stream, None
 
-    def __enter__(self):
-        if torch.cuda.current_device() != self.device.index:
-            self.guard = torch.cuda.device(self.device)
-            self.guard.__enter__()
-        if self.stream is not None:
-            _require(self.stream.device == self.device, "the stream must be on the device of the tensors")
-        self.handle = _stream(self.stream)
-        return self
+def _on(device: int):
+    """Makes a tensor's device the current one for a call."""
+    return _HERE if torch.cuda.current_device() == device else torch.cuda.device(device)
 
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
 
-    def made(self, *tensors):
-        if self.stream is not None:
-            for t in tensors:
-                t.record_stream(self.stream)
+def _stream_on(device: int, stream) -> int:
+    if stream is None:
+        return torch.cuda.current_stream(device).cuda_stream
+    if stream.device.index != device:
+        _refuse("the stream must be on the device of the tensors")
+    return stream.cuda_stream
+
+
+def _made(stream, *tensors):
+    """Tells tensors that were made for a call of a stream that is not the current one."""
+    if stream is not None:
+        for t in tensors:
+            t.record_stream(stream)
 
 
 def k_quantize_rows(x, hp=0, stream=None):
     """strait_k_quantize_rows of x fp16 [M][K] (rows may lie further apart); returns (codes int8 [M][K], scale fp32 [M])."""
-    pitch = _rows(x, None, "x")
-    m, k = x.shape
-    with _On(x.device, stream) as on:
-        q = torch.empty((m, k), dtype=torch.int8, device=x.device)
-        scale = torch.empty((m,), dtype=torch.float32, device=x.device)
-        on.made(q, scale)
-        _check(lib.strait_k_quantize_rows(on.handle, _dev(x), m, k, pitch, _dev(q), _dev(scale), hp))
+    pitch = _rows(x, None, -1, "x")
+    (m, k), device = x.shape, x.get_device()
+    with _on(device):
+        handle = _stream_on(device, stream)
+        q, scale = torch.empty((m, k), dtype=torch.int8, device=x.device), torch.empty((m,), dtype=torch.float32, device=x.device)
+        _made(stream, q, scale)
+        _check(lib.strait_k_quantize_rows(handle, x.data_ptr(), m, k, pitch, q.data_ptr(), scale.data_ptr(), hp))
     return q, scale
 
 
 def k_gemm_i8(x, x_scale, w, w_scale, bias=None, act=ACT_NONE, res=None, out_f32=False, hp=0, stream=None):
     """strait_k_gemm_i8: x int8 [M][K] and its rows' scales, w int8 [N][K] and its rows' scales; returns y [M][N]."""
-    _operand(x, torch.int8, (None, None), "x")
-    m, k = x.shape
-    _operand(w, torch.int8, (None, k), "w", x.device)
-    n = w.shape[0]
-    _operand(x_scale, torch.float32, (m,), "x_scale", x.device)
-    _operand(w_scale, torch.float32, (n,), "w_scale", x.device)
+    _dense(x, torch.int8, (None, None), -1, "x")
+    (m, k), device = x.shape, x.get_device()
+    _dense(w, torch.int8, (None, k), device, "w")
+    n = w.size(0)
+    _dense(x_scale, torch.float32, (m,), device, "x_scale")
+    _dense(w_scale, torch.float32, (n,), device, "w_scale")
     if bias is not None:
-        _operand(bias, torch.float32, (n,), "bias", x.device)
+        _dense(bias, torch.float32, (n,), device, "bias")
     if res is not None:
-        _operand(res, torch.float16, (m, n), "res", x.device)
-    with _On(x.device, stream) as on:
+        _dense(res, torch.float16, (m, n), device, "res")
+    with _on(device):
+        handle = _stream_on(device, stream)
         y = torch.empty((m, n), dtype=torch.float32 if out_f32 else torch.float16, device=x.device)
-        on.made(y)
-        _check(lib.strait_k_gemm_i8(on.handle, _dev(x), _dev(x_scale), _dev(w), _dev(w_scale), _dev(bias), m, n, k, act, _dev(res), _dev(y), int(out_f32), hp))
+        _made(stream, y)
+        _check(lib.strait_k_gemm_i8(handle, x.data_ptr(), x_scale.data_ptr(), w.data_ptr(), w_scale.data_ptr(), _dev(bias), m, n, k, act, _dev(res), y.data_ptr(), out_f32, hp))
     return y
 
 
@@ -680,15 +681,16 @@ class KvCache:
     [pages][kv_heads]."""
 
     def __init__(self, k, v, k_scale=None, v_scale=None):
-        _require(torch.is_tensor(k) and k.dtype in (torch.float16, torch.int8), "k must be a float16 or int8 tensor")
-        _operand(k, k.dtype, (None,) * 4, "k")
-        _operand(v, k.dtype, tuple(k.shape), "v", k.device)
-        i8 = k.dtype == torch.int8
-        _require(i8 == (k_scale is not None) and i8 == (v_scale is not None), "an int8 cache has k_scale and v_scale, an fp16 cache none")
-        for t, what in ((k_scale, "k_scale"), (v_scale, "v_scale")):
-            if i8:
-                _operand(t, torch.float32, tuple(k.shape[:2]), what, k.device)
-        self.k, self.v, self.k_scale, self.v_scale, self.device = k, v, k_scale, v_scale, k.device
+        i8 = isinstance(k, torch.Tensor) and k.dtype is torch.int8
+        _dense(k, torch.int8 if i8 else torch.float16, (None,) * 4, -1, "k")
+        self.device = k.get_device()
+        _dense(v, k.dtype, tuple(k.shape), self.device, "v")
+        if i8 != (k_scale is not None) or i8 != (v_scale is not None):
+            _refuse("an int8 cache has k_scale and v_scale, an fp16 cache none")
+        if i8:
+            _dense(k_scale, torch.float32, tuple(k.shape[:2]), self.device, "k_scale")
+            _dense(v_scale, torch.float32, tuple(k.shape[:2]), self.device, "v_scale")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.pages, self.kv_heads, self.page_tokens, self.head_dim = k.shape
         self.desc = KvCacheDesc(_dev(k), _dev(v), _dev(k_scale), _dev(v_scale), KV_I8 if i8 else KV_F16, self.pages, self.page_tokens, self.kv_heads, self.head_dim)
         self.ref = C.byref(self.desc)
@@ -699,10 +701,11 @@ class KvBatch:
     [seqs][columns].  How many tokens a step has is the rows of the tensors that it is called with."""
 
     def __init__(self, q_start, kv_len, page_table, max_q: int, max_kv: int):
-        _operand(kv_len, torch.int32, (None,), "kv_len")
-        _operand(q_start, torch.int32, (kv_len.shape[0] + 1,), "q_start", kv_len.device)
-        _operand(page_table, torch.int32, (kv_len.shape[0], None), "page_table", kv_len.device)
-        self.q_start, self.kv_len, self.page_table, self.device = q_start, kv_len, page_table, kv_len.device
+        _dense(kv_len, torch.int32, (None,), -1, "kv_len")
+        self.device = kv_len.get_device()
+        _dense(q_start, torch.int32, (kv_len.shape[0] + 1,), self.device, "q_start")
+        _dense(page_table, torch.int32, (kv_len.shape[0], None), self.device, "page_table")
+        self.q_start, self.kv_len, self.page_table = q_start, kv_len, page_table
         self.desc = KvBatchDesc(_dev(q_start), _dev(kv_len), _dev(page_table), kv_len.shape[0], 0, max_q, max_kv, page_table.shape[1])
         self._of = {}
 
@@ -721,51 +724,59 @@ class KvBatch:
 def k_kv_append(cache: KvCache, batch: KvBatch, k, v, q=None, rope=None, interleaved=False, q_out=None, hp=0, stream=None):
     """strait_k_kv_append of k, v fp16 [tokens][kv_heads * head_dim] (rows may lie further apart: columns of a fused projection's output); with q
     [tokens][heads * head_dim], returns the rotated queries (in q_out, if given).  rope: rope_table() on the device."""
-    _require(cache.device == batch.device, "cache and batch must be on one device")
-    width = cache.kv_heads * cache.head_dim
-    pk, pv = _rows(k, width, "k", cache.device), _rows(v, width, "v", cache.device)
-    tokens = k.shape[0]
-    _require(v.shape[0] == tokens, "k and v have different numbers of tokens")
-    pq = heads = 0
+    device, dim = cache.device, cache.head_dim
+    if batch.device != device:
+        _refuse("cache and batch must be on one device")
+    width = cache.kv_heads * dim
+    pk, pv = _rows(k, width, device, "k"), _rows(v, width, device, "v")
+    tokens, pq, heads, rope_rows, rope_dim = k.size(0), 0, 0, 0, 0
+    if v.size(0) != tokens:
+        _refuse("k and v have different numbers of tokens")
     if rope is not None:
-        _operand(rope, torch.float32, (None, None), "rope", cache.device)
-    _require(q is not None or q_out is None, "q_out without q")
-    with _On(cache.device, stream) as on:
-        if q is not None:
-            pq = _rows(q, None, "q", cache.device)
-            _require(q.shape[0] == tokens and q.shape[1] % cache.head_dim == 0, "q must be [tokens][heads * head_dim]")
-            heads = q.shape[1] // cache.head_dim
-            if q_out is None:
-                q_out = torch.empty((tokens, q.shape[1]), dtype=torch.float16, device=q.device)
-                on.made(q_out)
-            else:
-                _operand(q_out, torch.float16, tuple(q.shape), "q_out", cache.device)
-        _check(lib.strait_k_kv_append(on.handle, cache.ref, batch.ref(tokens), _dev(q), _dev(k), _dev(v), pq, pk, pv, heads, _dev(rope),
-                                      0 if rope is None else rope.shape[0], 0 if rope is None else rope.shape[1], int(interleaved), _dev(q_out), hp))
+        _dense(rope, torch.float32, (None, None), device, "rope")
+        rope_rows, rope_dim = rope.shape
+    if q is not None:
+        pq, heads = _rows(q, None, device, "q"), q.size(1) // dim
+        if q.size(0) != tokens or q.size(1) != heads * dim:
+            _refuse(f"q must be [{tokens}][heads * {dim}], is {tuple(q.shape)}")
+    elif q_out is not None:
+        _refuse("q_out without q")
+    with _on(device):
+        handle = _stream_on(device, stream)
+        if q_out is not None:
+            _dense(q_out, torch.float16, (tokens, heads * dim), device, "q_out")
+        elif q is not None:
+            q_out = torch.empty((tokens, heads * dim), dtype=torch.float16, device=q.device)
+            _made(stream, q_out)
+        _check(lib.strait_k_kv_append(handle, cache.ref, batch.ref(tokens), _dev(q), k.data_ptr(), v.data_ptr(), pq, pk, pv, heads, _dev(rope), rope_rows, rope_dim,
+                                      interleaved, _dev(q_out), hp))
     return q_out
 
 
 def k_attention_paged(q, cache: KvCache, batch: KvBatch, scale: float, window: int = 0, sinks: int = 0, out=None, hp=0, stream=None):
     """strait_k_attention_paged of q fp16 [tokens][heads * head_dim] (rows may lie further apart); returns out, of the same shape (rows that belong to no
     sequence are left as they are: of a tensor made here, undefined)."""
-    _require(cache.device == batch.device, "cache and batch must be on one device")
-    pitch = _rows(q, None, "q", cache.device)
+    device, dim = cache.device, cache.head_dim
+    if batch.device != device:
+        _refuse("cache and batch must be on one device")
+    pitch = _rows(q, None, device, "q")
     tokens, width = q.shape
-    _require(width % cache.head_dim == 0, "q must be [tokens][heads * head_dim]")
-    heads = width // cache.head_dim
-    with _On(cache.device, stream) as on:
+    heads = width // dim
+    if heads * dim != width:
+        _refuse(f"q must be [tokens][heads * {dim}], is {tuple(q.shape)}")
+    with _on(device):
+        handle = _stream_on(device, stream)
         if out is None:
             out = torch.empty((tokens, width), dtype=torch.float16, device=q.device)
-            on.made(out)
+            _made(stream, out)
         else:
-            _operand(out, torch.float16, (tokens, width), "out", cache.device)
-        need, ref = _sz(), batch.ref(tokens)
+            _dense(out, torch.float16, (tokens, width), device, "out")
+        need, ref, ws = _sz(), batch.ref(tokens), None
         _check(lib.strait_k_attention_paged_workspace(cache.ref, ref, heads, window, sinks, C.byref(need)))
-        ws = None
         if need.value:
             ws = torch.empty((need.value,), dtype=torch.uint8, device=q.device)
-            on.made(ws)
-        _check(lib.strait_k_attention_paged(on.handle, cache.ref, ref, _dev(q), pitch, heads, scale, window, sinks, _dev(out), _dev(ws), need.value, hp))
+            _made(stream, ws)
+        _check(lib.strait_k_attention_paged(handle, cache.ref, ref, q.data_ptr(), pitch, heads, scale, window, sinks, out.data_ptr(), _dev(ws), need.value, hp))
     return out
 
 

@@ -2,13 +2,22 @@
 //
 //   y[m, n] = act( xs[m] ws[n] sum_k x[m, k] w[n, k] + bias[n] (+ res[m, n]) )
 //
-// The sum is an int32 of v_mfma_i32_32x32x32_i8 and exact; the epilogue is fp32, rounded once.
+// The sum is an int32 of the integer MFMAs and exact in any order; the epilogue is fp32, rounded once.  Two kernels:
+//
+//   gemm_i8_stream_kernel, up to 64 rows: bound by the weights' bytes.  A workgroup of 8 wavefronts has 16 NT channels and shares the reduction
+//   out in pieces of 256; weights go from memory to registers in the layout of v_mfma_i32_16x16x64_i8's operand, a piece ahead, and each byte is read
+//   once on the whole chip.  The partial sums meet in LDS as integers.
+//
+//   gemm_i8_tile_kernel: bound by the matrix pipes.  Slices of 64 of the reduction travel to a ring in LDS without passing through registers, the operands of
+//   the next MFMAs are read while the current ones run, and one barrier per slice hands a stage on.
+#include <type_traits>
+
 #include "activation.hpp"
+#include "conv_dma.hpp"
 #include "decoder.hpp"
 
 namespace strait {
 
-typedef int intx4 __attribute__((ext_vector_type(4)));
 typedef int intx16 __attribute__((ext_vector_type(16)));
 
 // One output of a sum: the same operations in the same order in every kernel, so that a row has the same bits whatever launch it is part of.
@@ -16,36 +25,248 @@ __device__ __forceinline__ float finish(int sum, float xs, float ws, float bias,
     return apply_act(__builtin_fmaf((float)sum, xs * ws, bias) + res, act);
 }
 
-__global__ void __launch_bounds__(256) gemm_i8_kernel(const GemmI8 p, int tiles_n) {
+// ---- few rows -------------------------------------------------------------------------------------------------------
+
+constexpr int STREAM_WAVES = 8, STREAM_STEPS = 4;      // steps of 64 in a piece
+
+template <int MT, int NT>
+__global__ void __launch_bounds__(64 * STREAM_WAVES) gemm_i8_stream_kernel(const GemmI8 p) {
+    __shared__ int sums[16 * MT][16 * NT];
     if (p.hp) __builtin_amdgcn_s_setprio(3);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, lh = lane >> 5;
-    const int tm = (int)blockIdx.x / tiles_n, tn = (int)blockIdx.x - tm * tiles_n;
-    const int m = tm * 64 + (wave >> 1) * 32 + l32, n0 = tn * 64 + (wave & 1) * 32, n = n0 + l32;
-    const int8_t* xr = p.x + (long long)(m < p.M ? m : p.M - 1) * p.K + lh * 16;
-    const int8_t* wr = p.w + (long long)(n < p.N ? n : p.N - 1) * p.K + lh * 16;
-    intx16 acc = {};
-    for (int k = 0; k < p.K; k += 32) {
-        const bool there = k + lh * 16 < p.K;
-        const intx4 a = there ? *(const intx4*)(wr + k) : intx4{}, b = there ? *(const intx4*)(xr + k) : intx4{};
-        acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, acc, 0, 0, 0);
-    }
-    if (m >= p.M) return;
-    // lane holds y[m][n0 + 8 g + 4 lh + j], v = 4 g + j
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l16 = lane & 15, g4 = lane >> 4;
+    const int n0 = (int)blockIdx.x * 16 * NT, m0 = (int)blockIdx.y * 16 * MT;
+    constexpr int PIECE = 64 * STREAM_STEPS;
+    const int pieces = (p.K + PIECE - 1) / PIECE;
+    const int8_t* wr[NT];
+    const int8_t* xr[MT];
 #pragma unroll
-    for (int v = 0; v < 16; ++v) {
-        const int c = n0 + 8 * (v >> 2) + 4 * lh + (v & 3);
-        if (c >= p.N) continue;
-        const long long at = (long long)m * p.N + c;
-        const float y = finish(acc[v], p.xs[m], p.ws[c], p.bias ? p.bias[c] : 0.f, p.res ? (float)p.res[at] : 0.f, p.act);
-        if (p.out_f32) ((float*)p.y)[at] = y;
-        else ((half_t*)p.y)[at] = (half_t)y;
+    for (int t = 0; t < NT; ++t) wr[t] = p.w + (long long)(n0 + 16 * t + l16 < p.N ? n0 + 16 * t + l16 : p.N - 1) * p.K;    // (rows past the end: the last one, not stored)
+#pragma unroll
+    for (int t = 0; t < MT; ++t) xr[t] = p.x + (long long)(m0 + 16 * t + l16 < p.M ? m0 + 16 * t + l16 : p.M - 1) * p.K;
+    auto at = [&](const int8_t* row, int piece, int s) __attribute__((always_inline)) {
+        const int k = piece * PIECE + 64 * s + 16 * g4;
+        return k < p.K ? *(const intx4*)(row + k) : intx4{0, 0, 0, 0};
+    };
+    intx4 acc[NT][MT] = {};
+    intx4 w[NT][STREAM_STEPS], x[MT][STREAM_STEPS];
+    auto load = [&](int piece) __attribute__((always_inline)) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int s = 0; s < STREAM_STEPS; ++s) w[t][s] = at(wr[t], piece, s);
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+            for (int s = 0; s < STREAM_STEPS; ++s) x[t][s] = at(xr[t], piece, s);
+    };
+    if (wave < pieces) load(wave);
+    for (int i = threadIdx.x; i < 256 * MT * NT; i += 64 * STREAM_WAVES) (&sums[0][0])[i] = 0;
+    for (int piece = wave; piece < pieces; piece += STREAM_WAVES) {
+        intx4 wc[NT][STREAM_STEPS], xc[MT][STREAM_STEPS];
+#pragma unroll
+        for (int s = 0; s < STREAM_STEPS; ++s) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t) wc[t][s] = w[t][s];
+#pragma unroll
+            for (int t = 0; t < MT; ++t) xc[t][s] = x[t][s];
+        }
+        if (piece + STREAM_WAVES < pieces) load(piece + STREAM_WAVES);
+#pragma unroll
+        for (int s = 0; s < STREAM_STEPS; ++s)
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int u = 0; u < MT; ++u) acc[t][u] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wc[t][s], xc[u][s], acc[t][u], 0, 0, 0);
+    }
+    __syncthreads();
+    // lane holds row l16 against channels 4 g4 .. + 3
+    if (wave < pieces) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int u = 0; u < MT; ++u)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) atomicAdd(&sums[16 * u + l16][16 * t + 4 * g4 + v], acc[t][u][v]);     // (integers: the order is of no account)
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 256 * MT * NT; i += 64 * STREAM_WAVES) {
+        const int r = i / (16 * NT), c = i - r * (16 * NT), m = m0 + r, n = n0 + c;
+        if (m >= p.M || n >= p.N) continue;
+        const long long o = (long long)m * p.N + n;
+        const float y = finish(sums[r][c], p.xs[m], p.ws[n], p.bias ? p.bias[n] : 0.f, p.res ? (float)p.res[o] : 0.f, p.act);
+        if (p.out_f32) ((float*)p.y)[o] = y;
+        else ((half_t*)p.y)[o] = (half_t)y;
     }
 }
 
+// ---- tiles ------------------------------------------------------------------------------------------------------------
+
+struct TileArgs { GemmI8 g; TileOrder order; };
+
+template <int BM, int BN, int WGM, int WGN, int STAGES>
+constexpr unsigned tile_lds() {
+    const unsigned ring = STAGES * (BM + BN) * 64, out = BM * (BN + 8) * 2;
+    return ring > out ? ring : out;
+}
+template <int BM, int BN, int WGM, int WGN, int STAGES>
+constexpr int tile_waves_per_simd() {
+    const int w = 160 * 1024 / (int)tile_lds<BM, BN, WGM, WGN, STAGES>() * WGM * WGN / 4;
+    return w < 1 ? 1 : w > 4 ? 4 : w;
+}
+
+template <int BM, int BN, int WGM, int WGN, int STAGES>
+__global__ void __launch_bounds__(64 * WGM * WGN, (tile_waves_per_simd<BM, BN, WGM, WGN, STAGES>())) gemm_i8_tile_kernel(const TileArgs a) {
+    const GemmI8& p = a.g;
+    constexpr int NW = WGM * WGN, NT = 64 * NW;
+    constexpr int TM = BM / WGM, TN = BN / WGN, TMB = TM / 32, TNB = TN / 32;
+    constexpr int XI = BM / (16 * NW), WI = BN / (16 * NW), NX = XI + WI, NM = TMB * TNB;    // transfers of 16 rows per wavefront and slice; MFMAs per step
+    constexpr unsigned STAGE = (BM + BN) * 64;
+    constexpr int LDC = BN + 8;
+    static_assert(TM % 32 == 0 && TN % 32 == 0 && BM % (16 * NW) == 0 && BN % (16 * NW) == 0 && STAGES >= 3 && tile_lds<BM, BN, WGM, WGN, STAGES>() <= 160 * 1024, "tile");
+
+    extern __shared__ __attribute__((aligned(1024))) char tile_smem[];
+    if (p.hp) __builtin_amdgcn_s_setprio(3);
+    const unsigned lds0 = (unsigned)(uintptr_t)tile_smem;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, lh = lane >> 5;
+    const int wm0 = (wave % WGM) * TM, wn0 = (wave / WGM) * TN;
+    int tm, tn;
+    place_tile(a.order, xcd_range(a.order.tiles, blockIdx.x), tm, tn);
+    const int m0 = tm * BM, n0 = tn * BN;
+
+    // the tile's rows as buffers of their own: offsets stay below 256 * 131056 whatever the operands' size; rows and numbers past the end arrive as zeros
+    const intx4 xrsrc = make_rsrc(p.x + (long long)m0 * p.K, (unsigned)(p.M - m0 < BM ? p.M - m0 : BM) * (unsigned)p.K);
+    const intx4 wrsrc = make_rsrc(p.w + (long long)n0 * p.K, (unsigned)(p.N - n0 < BN ? p.N - n0 : BN) * (unsigned)p.K);
+    // lane i brings 16 bytes of row i / 4; LDS holds chunk c of a row r at c ^ (r / 4 % 4), so that 16 rows read at one chunk meet no bank twice
+    const int rsub = lane >> 2, cl = (lane & 3) ^ ((rsub >> 2) & 3);
+    unsigned xoff[XI], woff[WI];
+#pragma unroll
+    for (int j = 0; j < XI; ++j) xoff[j] = m0 + (j * NW + wave) * 16 + rsub < p.M ? (unsigned)((j * NW + wave) * 16 + rsub) * (unsigned)p.K + cl * 16 : OOB_OFFSET;
+#pragma unroll
+    for (int j = 0; j < WI; ++j) woff[j] = n0 + (j * NW + wave) * 16 + rsub < p.N ? (unsigned)((j * NW + wave) * 16 + rsub) * (unsigned)p.K + cl * 16 : OOB_OFFSET;
+    const int nk = (p.K + 63) / 64;
+    auto issue_one = [&](int stage, int slice, int j) __attribute__((always_inline)) {
+        const bool there = slice * 64 + cl * 16 < p.K;             // (the last slice may be ragged)
+        const unsigned at = lds0 + (unsigned)stage * STAGE;
+        if (j < XI) dma16(xrsrc, there ? xoff[j] : OOB_OFFSET, (unsigned)slice * 64u, at + (unsigned)((j * NW + wave) * 1024));
+        else dma16(wrsrc, there ? woff[j - XI] : OOB_OFFSET, (unsigned)slice * 64u, at + BM * 64u + (unsigned)(((j - XI) * NW + wave) * 1024));
+    };
+    intx16 acc[TNB][TMB] = {};
+    intx4 wf[2][TNB], xf[2][TMB];
+    auto load_frags = [&](int buf, int stage, int ks) __attribute__((always_inline)) {
+        const char* xs = tile_smem + stage * (int)STAGE;
+        const char* ws = xs + BM * 64;
+        const int pos = ((ks * 2 + lh) ^ ((l32 >> 2) & 3)) * 16;
+#pragma unroll
+        for (int i = 0; i < TNB; ++i) wf[buf][i] = *(const intx4*)(ws + (wn0 + i * 32 + l32) * 64 + pos);
+#pragma unroll
+        for (int i = 0; i < TMB; ++i) xf[buf][i] = *(const intx4*)(xs + (wm0 + i * 32 + l32) * 64 + pos);
+    };
+    // STAGES - 1 slices under way; slices past the end are requested as zeros, so that every wait counts the same
+#pragma unroll
+    for (int s = 0; s < STAGES - 1; ++s)
+#pragma unroll
+        for (int j = 0; j < NX; ++j) issue_one(s, s, j);
+    wait_loads_then_barrier<(STAGES - 2) * NX>();
+    load_frags(0, 0, 0);
+    int rd = 0, fill = STAGES - 1;
+    for (int kt = 0; kt < nk; ++kt) {
+        load_frags(1, rd, 1);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int q = 0; q < NM; ++q) {
+            acc[q / TMB][q % TMB] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf[0][q / TMB], xf[0][q % TMB], acc[q / TMB][q % TMB], 0, 0, 0);
+            constexpr int PER = (NX + NM - 1) / NM;
+#pragma unroll
+            for (int j = q * PER; j < (q + 1) * PER && j < NX; ++j) issue_one(fill, kt + STAGES - 1, j);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        wait_loads_then_barrier<(STAGES - 2) * NX>();          // slice kt + 1 is there, and everyone has read slice kt
+        fill = rd;
+        rd = rd + 1 == STAGES ? 0 : rd + 1;
+        load_frags(0, rd, 0);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int q = 0; q < NM; ++q) acc[q / TMB][q % TMB] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf[1][q / TMB], xf[1][q % TMB], acc[q / TMB][q % TMB], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");   // the zeros past the end have arrived: LDS is free
+
+    // ---- epilogue: a lane holds y[m][n .. n + 3] of 8 g + 4 lh; fp16 results leave through LDS, 16 bytes a lane
+    half_t* const out = (half_t*)tile_smem;
+#pragma unroll
+    for (int b = 0; b < TMB; ++b) {
+        const int mt = wm0 + b * 32 + l32, m = m0 + mt;
+        const float xs = m < p.M ? p.xs[m] : 0.f;
+        const long long row = (long long)m * p.N;
+#pragma unroll
+        for (int t = 0; t < TNB; ++t)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int nt = wn0 + t * 32 + 8 * g + 4 * lh, n = n0 + nt;
+                half4 h;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const bool real = m < p.M && n + j < p.N;
+                    const int c = n + j < p.N ? n + j : p.N - 1;
+                    const float y = finish(acc[t][b][4 * g + j], xs, p.ws[c], p.bias ? p.bias[c] : 0.f, p.res && real ? (float)p.res[row + n + j] : 0.f, p.act);
+                    if (p.out_f32) {
+                        if (real) ((float*)p.y)[row + n + j] = y;
+                    } else h[j] = (half_t)y;
+                }
+                if (!p.out_f32) *(half4*)(out + mt * LDC + nt) = h;
+            }
+    }
+    if (p.out_f32) return;
+    __syncthreads();
+    if (p.N % 8 == 0 && (reinterpret_cast<uintptr_t>(p.y) & 15) == 0) {
+        for (int i = tid; i < BM * (BN / 8); i += NT) {
+            const int r = i / (BN / 8), c = (i - r * (BN / 8)) * 8;
+            if (m0 + r < p.M && n0 + c < p.N) *(half8*)((half_t*)p.y + (long long)(m0 + r) * p.N + n0 + c) = *(const half8*)(out + r * LDC + c);
+        }
+    } else {
+        for (int i = tid; i < BM * BN; i += NT) {
+            const int r = i / BN, c = i - r * BN;
+            if (m0 + r < p.M && n0 + c < p.N) ((half_t*)p.y)[(long long)(m0 + r) * p.N + n0 + c] = out[r * LDC + c];
+        }
+    }
+}
+
+template <int BM, int BN, int WGM, int WGN, int STAGES>
+static int launch_tile(const GemmI8& p, hipStream_t stream) {
+    const long long tiles_m = (p.M + BM - 1LL) / BM, tiles_n = (p.N + BN - 1LL) / BN;
+    if (tiles_m * tiles_n > 0x3fffffffLL) { set_error("gemm_i8: grid too large"); return STRAIT_E_SHAPE; }
+    ConvParams order{};
+    set_tile_order(order, tiles_m, (int)tiles_n, BM, BN, 64, 1);
+    const TileArgs a{p, order.order};
+    constexpr unsigned lds = tile_lds<BM, BN, WGM, WGN, STAGES>();
+    auto kernel = gemm_i8_tile_kernel<BM, BN, WGM, WGN, STAGES>;
+    static std::atomic<bool> configured{false};        // (per tile; setting the attribute twice is harmless)
+    if (lds > 64 * 1024 && !configured.load(std::memory_order_acquire)) {
+        const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e != hipSuccess) { set_error("gemm_i8: cannot reserve %u bytes of LDS: %s", lds, hipGetErrorString(e)); return STRAIT_E_HIP; }
+        configured.store(true, std::memory_order_release);
+    }
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(tiles_m * tiles_n)), dim3(64 * WGM * WGN), lds, stream, a);
+    return 0;
+}
+template <int MT, int NT>
+static void launch_stream(const GemmI8& p, hipStream_t stream) {
+    hipLaunchKernelGGL((gemm_i8_stream_kernel<MT, NT>), dim3((unsigned)((p.N + 16LL * NT - 1) / (16 * NT)), (unsigned)((p.M + 16 * MT - 1) / (16 * MT))), dim3(64 * STREAM_WAVES), 0, stream, p);
+}
+
 int launch_gemm_i8(const GemmI8& p, hipStream_t stream) {
-    const long long tiles_m = (p.M + 63LL) / 64, tiles_n = (p.N + 63LL) / 64;
-    if (tiles_m * tiles_n > 0x7fffffffLL) { set_error("gemm_i8: grid too large"); return STRAIT_E_SHAPE; }
-    hipLaunchKernelGGL(gemm_i8_kernel, dim3((unsigned)(tiles_m * tiles_n)), dim3(256), 0, stream, p, (int)tiles_n);
+    int rc = 0;
+    if (p.M <= 64) {
+        const int mt = (p.M + 15) / 16, nt = p.N >= 16384 ? 4 : p.N >= 8192 ? 2 : 1;
+#define STRAIT_GO(MT) (nt == 4 ? launch_stream<MT, 4>(p, stream) : nt == 2 ? launch_stream<MT, 2>(p, stream) : launch_stream<MT, 1>(p, stream))
+        if (mt == 1) STRAIT_GO(1);
+        else if (mt == 2) STRAIT_GO(2);
+        else if (mt == 3) STRAIT_GO(3);
+        else STRAIT_GO(4);
+#undef STRAIT_GO
+    } else if ((p.M + 255LL) / 256 * ((p.N + 255LL) / 256) >= 256) rc = launch_tile<256, 256, 2, 4, 4>(p, stream);
+    else rc = launch_tile<128, 128, 2, 2, 4>(p, stream);
+    if (rc) return rc;
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) { set_error("gemm_i8 launch: %s", hipGetErrorString(e)); return -2; }
     return 0;
