@@ -2,8 +2,11 @@
 //
 //   out[t, h] = sum_j softmax_j( scale q[t, h] . k_j ) v_j  over the keys j <= p  with  window == 0  or  p - j < window  or  j < sinks
 //
-// The rows of a tile are 16 (token, head of the group) pairs of one kv head: all of them read the same keys.  A wavefront walks over the keys in
-// blocks of 32, which lie on one page each:
+// The rows of a tile are (token, head of the group) pairs of one kv head: all of them read the same keys.  The keys that any of them sees, in blocks of
+// 32 that lie on one page each, are shared out over workgroups (parts of `per_part` blocks, whose results a second launch joins) and over a workgroup's four
+// wavefronts, which take every fourth block:
+//   - a wavefront's page numbers and scales are fetched at once, a lane for each block, and named by v_readlane; the next block's bytes are on their way to
+//     registers while a block is worked on;
 //   - scores^T = K Q^T with v_mfma_f32_16x16x32_f16: a lane names 16 bytes of a key, as they lie in memory, and Q is enumerated in the same order; it then holds
 //     8 of the block's keys for ONE row;
 //   - an int8 code becomes fp16 by way of the number 2^-24 (code + 128), a subnormal whose bits are the code's: one fused multiply-add makes
@@ -12,18 +15,20 @@
 //     read 8 keys at D / 16 dimensions each and exchange bytes within a lane;
 //   - one pass with a running maximum, which follows the true one only where that is more than 8 (in log2) ahead: probabilities stay below 2^8, and the
 //     output is rescaled a few times in all.
+#include <algorithm>
+#include <type_traits>
+
 #include "decoder.hpp"
 
 namespace strait {
 
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
-typedef _Float16 half4 __attribute__((ext_vector_type(4)));
 typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
-typedef unsigned uintx2 __attribute__((ext_vector_type(2)));
 
 constexpr int KEYS = 32;                 // of a block
+constexpr int PAGED_WAVES = 4;
 
 // Two of the 8-bit codes in `a` and `b` (biased by 128: codes ^ 0x80) as fp16 code 2^-9; sel: v_perm_b32's selector of the two bytes
 __device__ __forceinline__ half2_t two_codes(unsigned a, unsigned b, unsigned sel) {
@@ -45,155 +50,373 @@ __device__ __forceinline__ Blocks visible_blocks(int lo, int hi, int window, int
     if (sink >= first) return {0, 0, last};            // one piece
     return {sink, first, sink + last - first};
 }
+// The most blocks that a tile of `rows` rows can see.
+static int most_blocks(const PagedAttention& p, int rows) {
+    const int all = (p.batch.max_kv + KEYS - 1) / KEYS;
+    if (!p.window) return all;
+    const int group = p.heads / p.cache.kv_heads, apart = (rows + group - 2) / group;      // positions of two rows
+    return (int)std::min<long long>(all, ((long long)apart + p.window - 1) / KEYS + 2 + (p.sinks + KEYS - 1) / KEYS);
+}
 
+struct PagedArgs {
+    PagedAttention p;
+    int group, tiles, rows;              // query heads of a kv head; tiles of a sequence's rows and head, rows of a tile
+    int per_part, parts;                 // blocks of a part, parts at most
+    float* o; float* ml;                 // of parts: [tokens heads][parts][D] and [..][2]: the output over the sum, the maximum and the sum
+    Divisor by_group, by_heads, by_seqs, by_tiles;
+};
+
+// A tile's rows: of sequence s, lo .. hi the positions of the first and last one.
+struct Tile { int r0, lo, hi; bool any; };
+__device__ __forceinline__ Tile tile_of(const PagedArgs& a, const Sequence& s, int tile) {
+    const int r0 = tile * a.rows, last = divide(r0 + a.rows - 1, a.by_group);
+    return {r0, s.past + divide(r0, a.by_group), s.past + (last < s.n ? last : s.n - 1), r0 < s.n * a.group};
+}
+
+// A block's bytes as they come from memory: keys 16 kb + l16 at 16-byte pieces of their dimensions, and the values of 8 keys at J dimensions.
 template <int D, bool I8>
-__global__ void __launch_bounds__(64) paged_attention_kernel(const PagedAttention p, int tiles) {
-    if (p.hp) __builtin_amdgcn_s_setprio(3);
-    const int lane = threadIdx.x, l16 = lane & 15, g4 = lane >> 4;
-    const int H = p.cache.kv_heads, P = p.cache.page_tokens, group = p.heads / H;
-    const int tile = (int)blockIdx.x % tiles, bh = (int)blockIdx.x / tiles, h = bh % H, b = bh / H;
-    const Sequence s = sequence(p.batch, b);
-    const int r0 = tile * 16;
-    if (r0 >= s.n * group) return;
-    const int r = r0 + l16, i = r / group;
-    const bool real = i < s.n;
-    const int pos = s.past + i;                        // of this lane's row
-    const int lo = s.past + r0 / group, hi_row = (r0 + 15) / group, hi = s.past + (hi_row < s.n ? hi_row : s.n - 1);
-    const Blocks blocks = visible_blocks(lo, hi, p.window, p.sinks);
-    const half_t* qrow = p.q + (long long)(s.first + (real ? i : 0)) * p.pitch_q + (h * group + (real ? r - i * group : 0)) * D;
-
-    // Q: dimension of element e of step t: int8 16 g4 + 64 (t / 2) + 8 (t % 2) + e, fp16 8 g4 + 32 t + e
-    half8 qf[D / 32];
+struct RawBlock {
+    static constexpr int KP = D * (I8 ? 1 : 2) / 64, VW = D / 16 * (I8 ? 1 : 2) / 4;       // pieces of a key per lane; words of a value
+    uintx4 k[2][KP];
+    unsigned v[8][VW];
+    __device__ __forceinline__ void load(const strait_kv_cache& c, int place, int row, int l16, int g4) {
+        const long long at = ((long long)place * c.page_tokens + row) * (D * (I8 ? 1 : 2));
+        const char* kp = (const char*)c.k + at;
+        const char* vp = (const char*)c.v + at;
 #pragma unroll
-    for (int t = 0; t < D / 32; ++t) qf[t] = *(const half8*)(qrow + (I8 ? 16 * g4 + 64 * (t >> 1) + 8 * (t & 1) : 8 * g4 + 32 * t));
-
-    constexpr int J = D / 16;
-    floatx4 o[J];
+        for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-    for (int j = 0; j < J; ++j) o[j] = floatx4{0.f, 0.f, 0.f, 0.f};
-    float m = -INFINITY, l = 0.f;
-    const float c = p.scale * 1.44269504088896340736f * (I8 ? 512.f : 1.f);
-
-    for (int n = 0; n < blocks.count; ++n) {
-        const int k0 = blocks.at(n) * KEYS;
-        const int page = p.batch.page_table[(long long)b * p.batch.table_pitch + k0 / P];
-        if ((unsigned)page >= (unsigned)p.cache.pages) continue;
-        const long long place = (long long)page * H + h;
-        const long long row0 = place * P + (k0 & (P - 1));
-        half8 kf[2][D / 32];
-        half8 vf[J];
-        if (I8) {
-            const int8_t* kp = (const int8_t*)p.cache.k + row0 * D;
-            const int8_t* vp = (const int8_t*)p.cache.v + row0 * D;
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                for (int u = 0; u < D / 64; ++u) {
-                    const uintx4 w = *(const uintx4*)(kp + (kb * 16 + l16) * D + 16 * g4 + 64 * u) ^ 0x80808080u;
-#pragma unroll
-                    for (int e = 0; e < 16; e += 2) {
-                        const half2_t x = two_codes(w[e >> 2], 0, e & 2 ? 0x0c030c02u : 0x0c010c00u);
-                        kf[kb][2 * u + (e >> 3)][e & 7] = x[0];
-                        kf[kb][2 * u + (e >> 3)][(e & 7) + 1] = x[1];
-                    }
-                }
-            unsigned w[8][J / 4];
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-#pragma unroll
-                for (int u = 0; u < J / 4; ++u) w[e][u] = *(const unsigned*)(vp + (16 * (e >> 2) + 4 * g4 + (e & 3)) * D + J * l16 + 4 * u) ^ 0x80808080u;
-#pragma unroll
-            for (int j = 0; j < J; ++j)
-#pragma unroll
-                for (int e = 0; e < 8; e += 2) {
-                    const half2_t x = two_codes(w[e][j >> 2], w[e + 1][j >> 2], 0x0c040c00u + 0x00010001u * (j & 3));
-                    vf[j][e] = x[0];
-                    vf[j][e + 1] = x[1];
-                }
-        } else {
-            const half_t* kp = (const half_t*)p.cache.k + row0 * D;
-            const half_t* vp = (const half_t*)p.cache.v + row0 * D;
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                for (int t = 0; t < D / 32; ++t) kf[kb][t] = *(const half8*)(kp + (kb * 16 + l16) * D + 8 * g4 + 32 * t);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int key = 16 * (e >> 2) + 4 * g4 + (e & 3);
-                // (a value that no row sees may be anything: 0 times an infinity is none of its business)
-                const bool seen = k0 + key <= hi && (!p.window || lo - (k0 + key) < p.window || k0 + key < p.sinks);
-                half_t v[J];
-#pragma unroll
-                for (int j = 0; j < J; ++j) v[j] = seen ? vp[key * D + J * l16 + j] : (half_t)0.f;
-#pragma unroll
-                for (int j = 0; j < J; ++j) vf[j][e] = v[j];
-            }
-        }
-        const float kc = I8 ? p.cache.k_scale[place] * c : c, vs = I8 ? p.cache.v_scale[place] * 512.f : 1.f;
-        float sc[8];                                   // keys k0 + 16 kb + 4 g4 + v, at e = 4 kb + v
-        float top = -INFINITY;
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            floatx4 a = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int t = 0; t < D / 32; ++t) a = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[kb][t], qf[t], a, 0, 0, 0);
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                const int key = k0 + 16 * kb + 4 * g4 + v;
-                const bool seen = key <= pos && (!p.window || pos - key < p.window || key < p.sinks);
-                sc[4 * kb + v] = seen ? a[v] * kc : -INFINITY;
-                top = fmaxf(top, sc[4 * kb + v]);
-            }
-        }
-        if (__any(top > m + 8.f)) {
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
-            const float now = fmaxf(m, top), alpha = now > -INFINITY ? __builtin_amdgcn_exp2f(m - now) : 1.f;
-            m = now;
-            l *= alpha;
-#pragma unroll
-            for (int j = 0; j < J; ++j) o[j] *= alpha;
-        }
-        const float ref = m > -INFINITY ? m : 0.f;
-        half8 pf;
+            for (int u = 0; u < KP; ++u) k[kb][u] = *(const uintx4*)(kp + (unsigned)((kb * 16 + l16) * KP * 64 + 16 * g4 + 64 * u));
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float v = __builtin_amdgcn_exp2f(sc[e] - ref);
-            l += v;
-            pf[e] = (half_t)v;
+            const char* src = vp + (unsigned)((16 * (e >> 2) + 4 * g4 + (e & 3)) * KP * 64 + l16 * VW * 4);
+            if constexpr (VW == 4) *(uintx4*)v[e] = *(const uintx4*)src;
+            else if constexpr (VW == 2) *(uint2*)v[e] = *(const uint2*)src;
+            else v[e][0] = *(const unsigned*)src;
+        }
+    }
+};
+
+template <int D, bool I8, int RT>
+__global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_stream_kernel(const PagedArgs a) {
+    constexpr int J = D / 16, LDO = D + 4;
+    __shared__ float so[2][RT * 16][LDO];
+    __shared__ float sml[2][RT * 16][2];
+    const PagedAttention& p = a.p;
+    if (p.hp) __builtin_amdgcn_s_setprio(3);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l16 = lane & 15, g4 = lane >> 4;
+    const int H = p.cache.kv_heads, P = p.cache.page_tokens;
+    // ((part tiles + tile) seqs + b) heads + h: every sequence's first part comes before any second one
+    const int i1 = divide((int)blockIdx.x, a.by_heads), h = (int)blockIdx.x - i1 * H, i2 = divide(i1, a.by_seqs), b = i1 - i2 * p.batch.seqs;
+    const int part = divide(i2, a.by_tiles), tile = i2 - part * a.tiles;
+    const Sequence s = sequence(p.batch, b);
+    const Tile t = tile_of(a, s, tile);
+    if (!t.any) return;
+    const Blocks blocks = visible_blocks(t.lo, t.hi, p.window, p.sinks);
+    const int begin = part * a.per_part, end = begin + a.per_part < blocks.count ? begin + a.per_part : blocks.count;
+    if (part && begin >= end) return;
+
+    // Q: dimension of element e of step u: int8 16 g4 + 64 (u / 2) + 8 (u % 2) + e, fp16 8 g4 + 32 u + e
+    half8 qf[RT][D / 32];
+    int pos[RT], head[RT], token[RT];                  // of this lane's rows
+#pragma unroll
+    for (int x = 0; x < RT; ++x) {
+        const int r = t.r0 + 16 * x + l16, i = divide(r, a.by_group);
+        head[x] = h * a.group + r - i * a.group;
+        token[x] = i < s.n ? s.first + i : -1;
+        pos[x] = s.past + i;
+        const half_t* qrow = p.q + (long long)(token[x] < 0 ? s.first : token[x]) * p.pitch_q + head[x] * D;
+#pragma unroll
+        for (int u = 0; u < D / 32; ++u) qf[x][u] = *(const half8*)(qrow + (I8 ? 16 * g4 + 64 * (u >> 1) + 8 * (u & 1) : 8 * g4 + 32 * u));
+    }
+    floatx4 o[RT][J];
+    float m[RT], l[RT];
+#pragma unroll
+    for (int x = 0; x < RT; ++x) {
+        m[x] = -INFINITY;
+        l[x] = 0.f;
+#pragma unroll
+        for (int j = 0; j < J; ++j) o[x][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+    const float c = p.scale * 1.44269504088896340736f * (I8 ? 512.f : 1.f);
+
+    auto work = [&](const RawBlock<D, I8>& raw, int k0, float kc, float vs, auto masked) __attribute__((always_inline)) {
+        constexpr bool MASK = decltype(masked)::value;
+        half8 kf[2][D / 32];
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int u = 0; u < RawBlock<D, I8>::KP; ++u) {
+                if constexpr (I8) {
+                    const uintx4 w = raw.k[kb][u] ^ 0x80808080u;
+#pragma unroll
+                    for (int e = 0; e < 16; e += 2) {
+                        const half2_t y = two_codes(w[e >> 2], 0, e & 2 ? 0x0c030c02u : 0x0c010c00u);
+                        kf[kb][2 * u + (e >> 3)][e & 7] = y[0];
+                        kf[kb][2 * u + (e >> 3)][(e & 7) + 1] = y[1];
+                    }
+                } else kf[kb][u] = __builtin_bit_cast(half8, raw.k[kb][u]);
+            }
+        half8 pf[RT];
+#pragma unroll
+        for (int x = 0; x < RT; ++x) {
+            float sc[8];                               // keys k0 + 16 kb + 4 g4 + v, at e = 4 kb + v
+            float top = -INFINITY;
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+                floatx4 d = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int u = 0; u < D / 32; ++u) d = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[kb][u], qf[x][u], d, 0, 0, 0);
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    const int key = k0 + 16 * kb + 4 * g4 + v;
+                    sc[4 * kb + v] = d[v] * kc;
+                    if (MASK && !(key <= pos[x] && (!p.window || pos[x] - key < p.window || key < p.sinks))) sc[4 * kb + v] = -INFINITY;
+                    top = fmaxf(top, sc[4 * kb + v]);
+                }
+            }
+            if (__any(top > m[x] + 8.f)) {
+                top = fmaxf(top, __shfl_xor(top, 16));
+                top = fmaxf(top, __shfl_xor(top, 32));
+                const float now = fmaxf(m[x], top), alpha = now > -INFINITY ? __builtin_amdgcn_exp2f(m[x] - now) : 1.f;
+                m[x] = now;
+                l[x] *= alpha;
+#pragma unroll
+                for (int j = 0; j < J; ++j) o[x][j] *= alpha;
+            }
+            const float ref = m[x] > -INFINITY ? m[x] : 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float v = __builtin_amdgcn_exp2f(sc[e] - ref);
+                l[x] += v;
+                pf[x][e] = (half_t)v;
+            }
+        }
+        unsigned w[8][RawBlock<D, I8>::VW];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            // (a value that no row sees may be anything: 0 times an infinity is none of its business)
+            const int key = k0 + 16 * (e >> 2) + 4 * g4 + (e & 3);
+            const bool seen = !MASK || I8 || (key <= t.hi && (!p.window || t.lo - key < p.window || key < p.sinks));
+#pragma unroll
+            for (int u = 0; u < RawBlock<D, I8>::VW; ++u) w[e][u] = I8 ? raw.v[e][u] ^ 0x80808080u : seen ? raw.v[e][u] : 0u;
         }
 #pragma unroll
         for (int j = 0; j < J; ++j) {
-            if (I8) {
-                const floatx4 a = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[j], pf, floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+            half8 vf;
 #pragma unroll
-                for (int v = 0; v < 4; ++v) o[j][v] = __builtin_fmaf(a[v], vs, o[j][v]);
-            } else o[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[j], pf, o[j], 0, 0, 0);
+            for (int e = 0; e < 8; e += 2) {
+                half2_t y;
+                if constexpr (I8) y = two_codes(w[e][j >> 2], w[e + 1][j >> 2], 0x0c040c00u + 0x00010001u * (j & 3));
+                else y = __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(w[e + 1][j >> 1], w[e][j >> 1], j & 1 ? 0x07060302u : 0x05040100u));
+                vf[e] = y[0];
+                vf[e + 1] = y[1];
+            }
+#pragma unroll
+            for (int x = 0; x < RT; ++x) {
+                if constexpr (I8) {
+                    const floatx4 d = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[x], floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) o[x][j][v] = __builtin_fmaf(d[v], vs, o[x][j][v]);
+                } else o[x][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[x], o[x][j], 0, 0, 0);
+            }
+        }
+    };
+
+    // 64 of this wavefront's blocks at a time
+    for (int first = begin + wave; first < end; first += 64 * PAGED_WAVES) {
+        const int mine = first + PAGED_WAVES * lane;
+        int k0s = 0, places = -1;
+        float kcs = 0.f, vss = 0.f;
+        if (mine < end) {
+            k0s = blocks.at(mine) * KEYS;
+            const int page = p.batch.page_table[(long long)b * p.batch.table_pitch + k0s / P];
+            if ((unsigned)page < (unsigned)p.cache.pages) {
+                places = page * H + h;
+                if (I8) { kcs = p.cache.k_scale[places] * c; vss = p.cache.v_scale[places] * 512.f; }
+            }
+        }
+        unsigned long long left = __ballot(places >= 0);
+        if (!left) continue;
+        RawBlock<D, I8> next;
+        int ni = __builtin_ctzll(left);
+        auto fetch = [&]() __attribute__((always_inline)) {
+            next.load(p.cache, __builtin_amdgcn_readlane(places, ni), __builtin_amdgcn_readlane(k0s, ni) & (P - 1), l16, g4);
+        };
+        fetch();
+        while (left) {
+            const RawBlock<D, I8> raw = next;
+            const int i = ni;
+            left &= left - 1;
+            if (left) {
+                ni = __builtin_ctzll(left);
+                fetch();
+            }
+            const int k0 = __builtin_amdgcn_readlane(k0s, i);
+            const float kc = I8 ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, kcs), i)) : c;
+            const float vs = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, vss), i));
+            if (k0 + KEYS - 1 <= t.lo && (!p.window || t.hi - k0 < p.window || k0 + KEYS - 1 < p.sinks)) work(raw, k0, kc, vs, std::false_type{});
+            else work(raw, k0, kc, vs, std::true_type{});
         }
     }
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
-    const float inv = l == 0.f ? 0.f : 1.f / l;        // nothing seen: zeros
-    if (!real) return;
-    half_t* orow = p.out + ((long long)(s.first + i) * p.heads + h * group + r - i * group) * D;
-    // lane holds row l16's dimensions J (4 g4 + v) + j
 #pragma unroll
-    for (int v = 0; v < 4; ++v)
+    for (int x = 0; x < RT; ++x) {
+        l[x] += __shfl_xor(l[x], 16);
+        l[x] += __shfl_xor(l[x], 32);
+    }
+    // four wavefronts' results become one: 2 and 3 hand theirs to 0 and 1, then 1 to 0; a lane holds row l16's dimensions J (4 g4 + v) + j
+    auto put = [&](int slot) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < J; ++j) orow[J * (4 * g4 + v) + j] = (half_t)(o[j][v] * inv);
+        for (int x = 0; x < RT; ++x) {
+            float* row = so[slot][16 * x + l16];
+#pragma unroll
+            for (int v = 0; v < 4; ++v)
+#pragma unroll
+                for (int j = 0; j < J; j += 4) *(floatx4*)(row + J * (4 * g4 + v) + j) = floatx4{o[x][j][v], o[x][j + 1][v], o[x][j + 2][v], o[x][j + 3][v]};
+            if (g4 == 0) { sml[slot][16 * x + l16][0] = m[x]; sml[slot][16 * x + l16][1] = l[x]; }
+        }
+    };
+    auto take = [&](int slot) __attribute__((always_inline)) {
+#pragma unroll
+        for (int x = 0; x < RT; ++x) {
+            const float m2 = sml[slot][16 * x + l16][0], l2 = sml[slot][16 * x + l16][1], now = fmaxf(m[x], m2);
+            const float a1 = m[x] > -INFINITY ? __builtin_amdgcn_exp2f(m[x] - now) : 0.f, a2 = m2 > -INFINITY ? __builtin_amdgcn_exp2f(m2 - now) : 0.f;
+            m[x] = now;
+            l[x] = l[x] * a1 + l2 * a2;
+            const float* row = so[slot][16 * x + l16];
+#pragma unroll
+            for (int v = 0; v < 4; ++v)
+#pragma unroll
+                for (int j = 0; j < J; j += 4) {
+                    const floatx4 y = *(const floatx4*)(row + J * (4 * g4 + v) + j);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) o[x][j + k][v] = o[x][j + k][v] * a1 + y[k] * a2;
+                }
+        }
+    };
+    if (wave >= 2) put(wave - 2);
+    __syncthreads();
+    if (wave < 2) take(wave);
+    __syncthreads();
+    if (wave == 1) put(0);
+    __syncthreads();
+    if (wave) return;
+    take(0);
+    const bool whole = blocks.count <= a.per_part;
+#pragma unroll
+    for (int x = 0; x < RT; ++x) {
+        if (token[x] < 0) continue;
+        const float inv = l[x] == 0.f ? 0.f : 1.f / l[x];      // nothing seen: zeros
+        const long long row = (long long)token[x] * p.heads + head[x];
+        if (whole) {
+            half_t* out = p.out + row * D;
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                half_t y[J];
+#pragma unroll
+                for (int j = 0; j < J; ++j) y[j] = (half_t)(o[x][j][v] * inv);
+                if constexpr (J == 8) *(uintx4*)(out + J * (4 * g4 + v)) = *(const uintx4*)y;
+                else *(uint2*)(out + J * (4 * g4 + v)) = *(const uint2*)y;
+            }
+        } else {
+            const long long slot = row * a.parts + part;
+            float* out = a.o + slot * D;
+#pragma unroll
+            for (int v = 0; v < 4; ++v)
+#pragma unroll
+                for (int j = 0; j < J; j += 4) *(floatx4*)(out + J * (4 * g4 + v) + j) = floatx4{o[x][j][v], o[x][j + 1][v], o[x][j + 2][v], o[x][j + 3][v]} * inv;
+            if (g4 == 0) *(float2*)(a.ml + slot * 2) = make_float2(m[x], l[x]);
+        }
+    }
 }
 
-size_t paged_attention_workspace(const PagedAttention&) { return 0; }
+// Joins the parts of rows that were shared out: a wavefront per (token, head).
+template <int D>
+__global__ void __launch_bounds__(256) paged_join_kernel(const PagedArgs a) {
+    const PagedAttention& p = a.p;
+    if (p.hp) __builtin_amdgcn_s_setprio(3);
+    const int lane = threadIdx.x & 63;
+    const int item = __builtin_amdgcn_readfirstlane((int)blockIdx.x * 4 + ((int)threadIdx.x >> 6));
+    const int hq = item % p.heads, bi = item / p.heads, i = bi % p.batch.max_q, b = bi / p.batch.max_q;
+    if (b >= p.batch.seqs) return;
+    const Sequence s = sequence(p.batch, b);
+    if (i >= s.n) return;
+    const int g = hq - divide(hq, a.by_group) * a.group;
+    const Tile t = tile_of(a, s, (i * a.group + g) / a.rows);
+    const Blocks blocks = visible_blocks(t.lo, t.hi, p.window, p.sinks);
+    const int parts = (blocks.count + a.per_part - 1) / a.per_part;
+    if (parts <= 1) return;
+    const long long row = (long long)(s.first + i) * p.heads + hq;
+    const float2* ml = (const float2*)a.ml + row * a.parts;
+    const float* o = a.o + row * a.parts * D + lane * (D / 64);
+    float top = -INFINITY;
+    for (int x = lane; x < parts; x += 64) top = fmaxf(top, ml[x].x);
+#pragma unroll
+    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    float sum = 0.f, y[D / 64] = {};
+    for (int x0 = 0; x0 < parts; x0 += 64) {
+        const float2 v = x0 + lane < parts ? ml[x0 + lane] : make_float2(-INFINITY, 0.f);
+        const float mine = v.y == 0.f ? 0.f : v.y * __builtin_amdgcn_exp2f(v.x - top);     // (NaN stays NaN)
+        sum += mine;
+        const int n = parts - x0 < 64 ? parts - x0 : 64;
+#pragma unroll 4
+        for (int x = 0; x < n; ++x) {
+            const float w = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, mine), x));
+#pragma unroll
+            for (int j = 0; j < D / 64; ++j) y[j] = __builtin_fmaf(w, o[(long long)(x0 + x) * D + j], y[j]);
+        }
+    }
+#pragma unroll
+    for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    half_t* out = p.out + row * D + lane * (D / 64);
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) out[j] = (half_t)(y[j] * inv);
+}
+
+// How a call is launched: tiles of 16 or 32 rows, and parts of as many blocks as give each compute unit several workgroups.
+static PagedArgs paged_plan(const PagedAttention& p) {
+    PagedArgs a{};
+    a.p = p;
+    a.group = p.heads / p.cache.kv_heads;
+    const long long rows = (long long)p.batch.max_q * a.group;
+    a.rows = rows <= 16 ? 16 : 32;
+    a.tiles = (int)((rows + a.rows - 1) / a.rows);
+    const int most = most_blocks(p, a.rows);
+    const long long work = (long long)p.batch.seqs * p.cache.kv_heads * a.tiles * most;
+    const long long per = (work + 2047) / 2048;
+    a.per_part = (int)std::min<long long>(most, std::max<long long>(8, (per + PAGED_WAVES - 1) / PAGED_WAVES * PAGED_WAVES));
+    a.parts = (most + a.per_part - 1) / a.per_part;
+    a.by_group = divisor(a.group); a.by_heads = divisor(p.cache.kv_heads); a.by_seqs = divisor(p.batch.seqs); a.by_tiles = divisor(a.tiles);
+    a.ml = p.ws;
+    const size_t head = ((size_t)p.batch.tokens * p.heads * a.parts * 2 * sizeof(float) + 15) / 16 * 16;
+    a.o = (float*)((char*)p.ws + head);
+    return a;
+}
+
+size_t paged_attention_workspace(const PagedAttention& p) {
+    const PagedArgs a = paged_plan(p);
+    if (a.parts <= 1) return 0;
+    const size_t slots = (size_t)p.batch.tokens * p.heads * a.parts;
+    return (slots * 2 * sizeof(float) + 15) / 16 * 16 + slots * p.cache.head_dim * sizeof(float);
+}
+
+template <int RT>
+static auto stream_kernel(const PagedAttention& p) {
+    const bool i8 = p.cache.type == STRAIT_KV_I8;
+    return p.cache.head_dim == 64 ? (i8 ? paged_stream_kernel<64, true, RT> : paged_stream_kernel<64, false, RT>) : (i8 ? paged_stream_kernel<128, true, RT> : paged_stream_kernel<128, false, RT>);
+}
 
 int launch_paged_attention(const PagedAttention& p, hipStream_t stream) {
-    const int H = p.cache.kv_heads, group = p.heads / H;
-    const int tiles = (int)(((long long)p.batch.max_q * group + 15) / 16);
-    const long long grid = (long long)p.batch.seqs * H * tiles;
-    if (grid > 0x7fffffffLL) { set_error("attention_paged: grid too large"); return STRAIT_E_SHAPE; }
-    const bool i8 = p.cache.type == STRAIT_KV_I8;
-    auto kernel = p.cache.head_dim == 64 ? (i8 ? paged_attention_kernel<64, true> : paged_attention_kernel<64, false>)
-                                         : (i8 ? paged_attention_kernel<128, true> : paged_attention_kernel<128, false>);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64), 0, stream, p, tiles);
+    const PagedArgs a = paged_plan(p);
+    const long long grid = (long long)p.batch.seqs * p.cache.kv_heads * a.tiles * a.parts, joins = ((long long)p.batch.seqs * p.batch.max_q * p.heads + 3) / 4;
+    if (grid > 0x7fffffffLL || joins > 0x1fffffffLL) { set_error("attention_paged: grid too large"); return STRAIT_E_SHAPE; }
+    auto kernel = a.rows == 16 ? stream_kernel<1>(p) : stream_kernel<2>(p);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * PAGED_WAVES), 0, stream, a);
+    if (a.parts > 1) {
+        auto join = p.cache.head_dim == 64 ? paged_join_kernel<64> : paged_join_kernel<128>;
+        hipLaunchKernelGGL(join, dim3((unsigned)joins), dim3(256), 0, stream, a);
+    }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) { set_error("attention_paged launch: %s", hipGetErrorString(e)); return -2; }
     return 0;
