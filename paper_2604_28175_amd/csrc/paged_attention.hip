@@ -330,6 +330,268 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_stream_kernel(const
     }
 }
 
+// ---- many rows ----------------------------------------------------------------------------------------------------------
+
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef __fp16 fp16x4 __attribute__((ext_vector_type(4)));
+typedef unsigned uintx2 __attribute__((ext_vector_type(2)));
+
+// The value of this lane and of lane ^ 32: {lanes 0-31's, lanes 32-63's}.
+__device__ __forceinline__ float2 halves_of(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false);
+    const unsigned lo = r[0], hi = r[1];
+    return {__builtin_bit_cast(float, lo), __builtin_bit_cast(float, hi)};
+}
+
+constexpr int TILE_KEYS = 64;            // two blocks
+
+template <int D, bool I8, int NW>
+__global__ void __launch_bounds__(64 * NW, 2) paged_tile_kernel(const PagedArgs a) {
+    constexpr int NT = 64 * NW, ROW = D * 2, STAGE = 2 * TILE_KEYS * ROW;      // bytes of a row of K or V in LDS, of a stage
+    constexpr int ES = I8 ? 1 : 2, PER_ROW = D * ES / 16, HALF = TILE_KEYS * PER_ROW, NI = 2 * HALF / NT;   // 16-byte pieces in memory: of a row, of K; of a thread
+    static_assert(2 * HALF % NT == 0, "pieces");
+    extern __shared__ __attribute__((aligned(16))) char tile_lds[];    // two stages
+    const PagedAttention& p = a.p;
+    if (p.hp) __builtin_amdgcn_s_setprio(3);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, lh = lane >> 5;
+    const int H = p.cache.kv_heads, P = p.cache.page_tokens;
+    const int i1 = divide((int)blockIdx.x, a.by_heads), h = (int)blockIdx.x - i1 * H, i2 = divide(i1, a.by_seqs), b = i1 - i2 * p.batch.seqs;
+    const int part = divide(i2, a.by_tiles), tile = a.tiles - 1 - (i2 - part * a.tiles);      // the last tiles see the most keys and go first
+    const Sequence s = sequence(p.batch, b);
+    const Tile t = tile_of(a, s, tile);
+    if (!t.any) return;
+    const Blocks blocks = visible_blocks(t.lo, t.hi, p.window, p.sinks);
+    const int begin = part * a.per_part, end = begin + a.per_part < blocks.count ? begin + a.per_part : blocks.count;
+    if (part && begin >= end) return;
+
+    // this lane's row, and the positions that the wavefront's rows span
+    const int r0 = t.r0 + wave * 32, r = r0 + l32, i = divide(r, a.by_group), head = h * a.group + r - i * a.group;
+    const int token = i < s.n ? s.first + i : -1, pos = s.past + i;
+    const bool any = r0 < s.n * a.group;
+    const int lo = s.past + divide(r0, a.by_group), hi_i = divide(r0 + 31, a.by_group), hi = s.past + (hi_i < s.n ? hi_i : s.n - 1);
+    half8 qf[D / 16];
+    {
+        const half_t* qrow = p.q + (long long)(token < 0 ? s.first : token) * p.pitch_q + head * D;
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) qf[ks] = *(const half8*)(qrow + ks * 16 + lh * 8);
+    }
+    floatx16 o[D / 32];
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) o[db][v] = 0.f;
+    float m = -INFINITY, l = 0.f;
+    const float c = p.scale * 1.44269504088896340736f * (I8 ? 512.f : 1.f);
+
+    // ---- memory -> registers -> LDS.  Chunk q of 16 bytes of row r lies at q ^ (r % 16) for K (D = 64: r % 8), whose operand is 16 rows at one chunk, and at q ^ 2 (r % 4)
+    // (D = 64: q ^ the bits of r % 8 reversed) for V, whose operand is 4 rows at 2 chunks
+    auto kswz = [](int row) { return D == 128 ? row & 15 : row & 7; };
+    auto vswz = [](int row) { return D == 128 ? (row & 3) << 1 : ((row & 1) << 2) | (row & 2) | ((row >> 2) & 1); };
+    uintx4 raw[NI];
+    // a lane of each wavefront holds what is to be known of a block: where it begins, its place (-1: not seen), and its scales
+    int k0s = 0, places = -1;
+    float kcs = c, vpow = 1.f, vlog = 0.f, vinv = 1.f;
+    auto look_up = [&](int first) __attribute__((always_inline)) {
+        k0s = 0x7fffff00;
+        places = -1;
+        if (first + lane < end) {
+            const int k0 = blocks.at(first + lane) * KEYS, page = p.batch.page_table[(long long)b * p.batch.table_pitch + k0 / P];
+            if ((unsigned)page < (unsigned)p.cache.pages) {
+                k0s = k0;
+                places = page * H + h;
+                if (I8) {
+                    kcs = p.cache.k_scale[places] * c;
+                    // a value is code 2^(f - 9), exact in fp16, f between -15 and 15; the rest of its scale goes into the probabilities
+                    const float vs = p.cache.v_scale[places] * 512.f;
+                    vpow = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, vs) & 0x7f800000u);
+                    vpow = vs == 0.f ? 0.f : fminf(fmaxf(vpow, 0x1p-15f), 0x1p15f);
+                    const float ratio = vs == 0.f ? 1.f : vs / vpow;
+                    vlog = __builtin_amdgcn_logf(ratio);
+                    vinv = 1.f / ratio;
+                }
+            }
+        }
+    };
+    auto of_block = [](int v, int n) __attribute__((always_inline)) { return __builtin_amdgcn_readlane(v, n); };
+    auto of_blockf = [](float v, int n) __attribute__((always_inline)) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), n)); };
+    auto fetch = [&](int n) __attribute__((always_inline)) {       // blocks n and n + 1 of the 64 that were looked up
+#pragma unroll
+        for (int x = 0; x < NI; ++x) {
+            const int id = x * NT + tid, v = id >= HALF, rem = v ? id - HALF : id, row = rem / PER_ROW, piece = rem % PER_ROW;
+            const int blk = __builtin_amdgcn_readfirstlane(n + (row >> 5)), place = of_block(places, blk), k0 = of_block(k0s, blk), key = k0 + (row & 31);
+            // (what no row of the tile sees may be anything: it arrives as zeros)
+            const bool seen = place >= 0 && (I8 || (key <= t.hi && (!p.window || t.lo - key < p.window || key < p.sinks)));
+            raw[x] = uintx4{0, 0, 0, 0};
+            if (seen) raw[x] = *(const uintx4*)((const char*)(v ? p.cache.v : p.cache.k) + ((long long)place * P + (k0 & (P - 1))) * (D * ES) + (unsigned)((row & 31) * PER_ROW + piece) * 16u);
+        }
+    };
+    auto stage = [&](int n, int st) __attribute__((always_inline)) {
+#pragma unroll
+        for (int x = 0; x < NI; ++x) {
+            const int id = x * NT + tid, v = id >= HALF, rem = v ? id - HALF : id, row = rem / PER_ROW, piece = rem % PER_ROW;
+            char* dst = tile_lds + st * STAGE + v * (TILE_KEYS * ROW) + row * ROW;
+            const int swz = v ? vswz(row) : kswz(row);
+            if constexpr (I8) {
+                const uintx4 w = raw[x] ^ 0x80808080u;
+                const half_t by = (half_t)of_blockf(vpow, __builtin_amdgcn_readfirstlane(n + (row >> 5)));
+                half8 y[2];
+#pragma unroll
+                for (int e = 0; e < 16; e += 2) {
+                    half2_t z = two_codes(w[e >> 2], 0, e & 2 ? 0x0c030c02u : 0x0c010c00u);
+                    if (v) z = z * half2_t{by, by};
+                    y[e >> 3][e & 7] = z[0];
+                    y[e >> 3][(e & 7) + 1] = z[1];
+                }
+                *(half8*)(dst + ((2 * piece) ^ swz) * 16) = y[0];
+                *(half8*)(dst + ((2 * piece + 1) ^ swz) * 16) = y[1];
+            } else *(uintx4*)(dst + (piece ^ swz) * 16) = raw[x];
+        }
+    };
+
+    // V: lane i of a group of 16 names keys 4 lh + (i >> 2), dimensions 16 ((lane >> 4) & 1) + 4 (i & 3) .. + 3 of a 16-key step and 32 dimensions, and receives
+    // the step's keys 4 lh .. 4 lh + 3 of dimension 16 ((lane >> 4) & 1) + i
+    const unsigned lds0 = (unsigned)(uintptr_t)tile_lds;
+    const int i16 = lane & 15, vr = lh * 4 + (i16 >> 2);
+    unsigned vaddr[D / 32];
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+        vaddr[db] = lds0 + TILE_KEYS * ROW + vr * ROW + (((db * 4 + ((lane >> 4) & 1) * 2 + ((i16 & 3) >> 1)) ^ vswz(vr)) << 4) + (i16 & 1) * 8;
+    auto vread = [](unsigned at) { return __builtin_amdgcn_ds_read_tr16_b64_v4f16((__attribute__((address_space(3))) fp16x4*)(uintptr_t)at); };
+
+    auto work = [&](int n, int st, auto masked) __attribute__((always_inline)) {
+        constexpr bool MASK = decltype(masked)::value;
+        const char* ks0 = tile_lds + st * STAGE;
+        floatx16 sc[2];                                // lane holds its row against keys 32 kb + 8 g + 4 lh + j of the tile (v = 4 g + j)
+        float kc[2], top = -INFINITY;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            kc[kb] = I8 ? of_blockf(kcs, n + kb) : c;
+            const int k0 = of_block(k0s, n + kb);
+#pragma unroll
+            for (int v = 0; v < 16; ++v) sc[kb][v] = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < D / 16; ++ks)
+                sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const half8*)(ks0 + (kb * 32 + l32) * ROW + (((ks * 2 + lh) ^ kswz(l32)) << 4)), qf[ks], sc[kb], 0, 0, 0);
+            if (MASK) {
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    const int key = k0 + 8 * (v >> 2) + 4 * lh + (v & 3);
+                    sc[kb][v] = key <= pos && (!p.window || pos - key < p.window || key < p.sinks) ? sc[kb][v] * kc[kb] : -INFINITY;
+                    top = fmaxf(top, sc[kb][v]);
+                }
+                kc[kb] = 1.f;
+            } else {
+                float most = sc[kb][0];
+#pragma unroll
+                for (int v = 1; v < 16; ++v) most = fmaxf(most, sc[kb][v]);
+                top = fmaxf(top, most * kc[kb]);       // (scales are not negative)
+            }
+        }
+        if (__any(top > m + 8.f)) {
+            const float2 both = halves_of(top);
+            const float now = fmaxf(m, fmaxf(both.x, both.y)), alpha = now > -INFINITY ? __builtin_amdgcn_exp2f(m - now) : 1.f;
+            m = now;
+            l *= alpha;
+#pragma unroll
+            for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) o[db][v] *= alpha;
+        }
+        const float ref = m > -INFINITY ? m : 0.f;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            const float off = (I8 ? of_blockf(vlog, n + kb) : 0.f) - ref;
+            float sum = 0.f;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                half8 pf;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float pv = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[kb][8 * half + j], kc[kb], off));
+                    sum += pv;
+                    pf[j] = (half_t)pv;
+                }
+#pragma unroll
+                for (int db = 0; db < D / 32; ++db) {
+                    const unsigned at = vaddr[db] + (unsigned)(st * STAGE + (kb * 32 + half * 16) * ROW);
+                    const fp16x4 lo4 = vread(at), hi4 = vread(at + 8 * ROW);
+                    half8 vf;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) { vf[j] = (half_t)lo4[j]; vf[4 + j] = (half_t)hi4[j]; }
+                    o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pf, o[db], 0, 0, 0);
+                }
+            }
+            l = I8 ? __builtin_fmaf(sum, of_blockf(vinv, n + kb), l) : l + sum;
+        }
+    };
+
+    if (begin < end) {
+        look_up(begin);
+        fetch(0);
+        stage(0, 0);
+        __syncthreads();
+        int st = 0, n = 0;                             // tile of blocks n, n + 1 of those that were looked up
+        for (int first = begin; first < end;) {
+            const int k0 = of_block(k0s, n), k1 = of_block(k0s, n + 1);
+            const bool dead = of_block(places, n) < 0 && of_block(places, n + 1) < 0;
+            // what the wavefront's rows see of the two blocks
+            auto none = [&](int k) { return k > hi || (p.window && lo - (k + KEYS - 1) >= p.window && k >= p.sinks); };
+            auto full = [&](int k) { return k + KEYS - 1 <= lo && (!p.window || hi - k < p.window || k + KEYS - 1 < p.sinks); };
+            const bool skip = !any || dead || (none(k0) && none(k1)), whole = full(k0) && full(k1);
+            const int nn = n + 2;
+            const bool more = first + 2 < end;
+            // (a look-up replaces what the current tile still needs: it waits for the tile's end)
+            const bool ahead = more && nn < 64;
+            if (ahead) fetch(nn);
+            if (!skip) {
+                if (whole) work(n, st, std::false_type{});
+                else work(n, st, std::true_type{});
+            }
+            n = nn;
+            first += 2;
+            if (more) {
+                if (!ahead) {
+                    look_up(first);
+                    n = 0;
+                    fetch(0);
+                }
+                stage(n, st ^ 1);
+            }
+            __syncthreads();
+            st ^= 1;
+        }
+    }
+    const float2 ll = halves_of(l);
+    l = ll.x + ll.y;
+    if (!any) return;
+    const float inv = l == 0.f ? 0.f : 1.f / l;        // nothing seen: zeros
+    const bool whole = blocks.count <= a.per_part;
+    const long long row = (long long)(token < 0 ? 0 : token) * p.heads + head;
+    if (whole) {
+        half_t* out = p.out + row * D;
+        // lane holds dimensions db * 32 + 8 g + 4 lh + j of its row; after the exchange with lane ^ 32, 8 of one g
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+            for (int g = 0; g < 4; g += 2) {
+                half_t e[4], f[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) { e[j] = (half_t)(o[db][4 * g + j] * inv); f[j] = (half_t)(o[db][4 * g + 4 + j] * inv); }
+                const uintx2 eu = *(const uintx2*)e, fu = *(const uintx2*)f;
+                const auto x = __builtin_amdgcn_permlane32_swap(eu[0], fu[0], false, false);
+                const auto y = __builtin_amdgcn_permlane32_swap(eu[1], fu[1], false, false);
+                if (token >= 0) *(uintx4*)(out + db * 32 + 8 * (g + lh)) = uintx4{x[0], y[0], x[1], y[1]};
+            }
+    } else if (token >= 0) {
+        const long long slot = row * a.parts + part;
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) *(floatx4*)(a.o + slot * D + db * 32 + 8 * g + 4 * lh) = floatx4{o[db][4 * g], o[db][4 * g + 1], o[db][4 * g + 2], o[db][4 * g + 3]} * inv;
+        if (lh == 0) *(float2*)(a.ml + slot * 2) = make_float2(m, l);
+    }
+}
+
 // Joins the parts of rows that were shared out: a wavefront per (token, head).
 template <int D>
 __global__ void __launch_bounds__(256) paged_join_kernel(const PagedArgs a) {
@@ -359,7 +621,6 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const PagedArgs a) {
         const float mine = v.y == 0.f ? 0.f : v.y * __builtin_amdgcn_exp2f(v.x - top);     // (NaN stays NaN)
         sum += mine;
         const int n = parts - x0 < 64 ? parts - x0 : 64;
-#pragma unroll 4
         for (int x = 0; x < n; ++x) {
             const float w = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, mine), x));
 #pragma unroll
@@ -374,18 +635,21 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const PagedArgs a) {
     for (int j = 0; j < D / 64; ++j) out[j] = (half_t)(y[j] * inv);
 }
 
-// How a call is launched: tiles of 16 or 32 rows, and parts of as many blocks as give each compute unit several workgroups.
+// How a call is launched.  Up to 32 rows of a sequence and kv head: the stream kernel, tiles of 16 or 32 rows.  More: the tile kernel, 128 rows, or 256 where those
+// still give every compute unit one.  Parts of as many blocks as give each compute unit several workgroups (tile kernel: one).
 static PagedArgs paged_plan(const PagedAttention& p) {
     PagedArgs a{};
     a.p = p;
     a.group = p.heads / p.cache.kv_heads;
-    const long long rows = (long long)p.batch.max_q * a.group;
-    a.rows = rows <= 16 ? 16 : 32;
+    const long long rows = (long long)p.batch.max_q * a.group, pairs = (long long)p.batch.seqs * p.cache.kv_heads;
+    const bool stream = rows <= 32;
+    a.rows = rows <= 16 ? 16 : stream ? 32 : pairs * ((rows + 255) / 256) >= 256 ? 256 : 128;
     a.tiles = (int)((rows + a.rows - 1) / a.rows);
     const int most = most_blocks(p, a.rows);
-    const long long work = (long long)p.batch.seqs * p.cache.kv_heads * a.tiles * most;
-    const long long per = (work + 2047) / 2048;
-    a.per_part = (int)std::min<long long>(most, std::max<long long>(8, (per + PAGED_WAVES - 1) / PAGED_WAVES * PAGED_WAVES));
+    const long long work = pairs * a.tiles * most;
+    const long long per = (work + (stream ? 2047 : 511)) / (stream ? 2048 : 512);
+    a.per_part = (int)std::min<long long>(most, std::max<long long>(stream ? 8 : 16, (per + PAGED_WAVES - 1) / PAGED_WAVES * PAGED_WAVES));
+    if (!stream && pairs * a.tiles >= 256) a.per_part = most;
     a.parts = (most + a.per_part - 1) / a.per_part;
     a.by_group = divisor(a.group); a.by_heads = divisor(p.cache.kv_heads); a.by_seqs = divisor(p.batch.seqs); a.by_tiles = divisor(a.tiles);
     a.ml = p.ws;
@@ -401,18 +665,26 @@ size_t paged_attention_workspace(const PagedAttention& p) {
     return (slots * 2 * sizeof(float) + 15) / 16 * 16 + slots * p.cache.head_dim * sizeof(float);
 }
 
-template <int RT>
-static auto stream_kernel(const PagedAttention& p) {
-    const bool i8 = p.cache.type == STRAIT_KV_I8;
-    return p.cache.head_dim == 64 ? (i8 ? paged_stream_kernel<64, true, RT> : paged_stream_kernel<64, false, RT>) : (i8 ? paged_stream_kernel<128, true, RT> : paged_stream_kernel<128, false, RT>);
+template <int D, bool I8>
+static void launch_paged(const PagedArgs& a, unsigned grid, hipStream_t stream) {
+    if (a.rows <= 32) {
+        auto kernel = a.rows == 16 ? paged_stream_kernel<D, I8, 1> : paged_stream_kernel<D, I8, 2>;
+        hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * PAGED_WAVES), 0, stream, a);
+    } else {
+        constexpr unsigned lds = 2 * 2 * TILE_KEYS * D * 2;
+        static_assert(lds <= 64 * 1024, "what a kernel may have unasked");
+        if (a.rows == 256) hipLaunchKernelGGL((paged_tile_kernel<D, I8, 8>), dim3(grid), dim3(512), lds, stream, a);
+        else hipLaunchKernelGGL((paged_tile_kernel<D, I8, 4>), dim3(grid), dim3(256), lds, stream, a);
+    }
 }
 
 int launch_paged_attention(const PagedAttention& p, hipStream_t stream) {
     const PagedArgs a = paged_plan(p);
     const long long grid = (long long)p.batch.seqs * p.cache.kv_heads * a.tiles * a.parts, joins = ((long long)p.batch.seqs * p.batch.max_q * p.heads + 3) / 4;
     if (grid > 0x7fffffffLL || joins > 0x1fffffffLL) { set_error("attention_paged: grid too large"); return STRAIT_E_SHAPE; }
-    auto kernel = a.rows == 16 ? stream_kernel<1>(p) : stream_kernel<2>(p);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * PAGED_WAVES), 0, stream, a);
+    const bool i8 = p.cache.type == STRAIT_KV_I8;
+    if (p.cache.head_dim == 64) i8 ? launch_paged<64, true>(a, (unsigned)grid, stream) : launch_paged<64, false>(a, (unsigned)grid, stream);
+    else i8 ? launch_paged<128, true>(a, (unsigned)grid, stream) : launch_paged<128, false>(a, (unsigned)grid, stream);
     if (a.parts > 1) {
         auto join = p.cache.head_dim == 64 ? paged_join_kernel<64> : paged_join_kernel<128>;
         hipLaunchKernelGGL(join, dim3((unsigned)joins), dim3(256), 0, stream, a);
