@@ -402,7 +402,7 @@ strait_status strait_k_gemm_i8(void* stream, const int8_t* x, const float* x_sca
                                int32_t M, int32_t N, int32_t K, int32_t act, const void* res, void* y, int32_t out_f32, int32_t hp);
 
 /* A paged cache of keys and values: k, v [pages][kv_heads][page_tokens][head_dim], 16-byte aligned.  STRAIT_KV_F16: fp16 (the scales are not
- * looked at).  STRAIT_KV_I8: int8 codes, k_scale, v_scale fp32 [pages][kv_heads]; a code stands for code * scale of its page and head.
+ * looked at).  STRAIT_KV_I8: int8 codes, k_scale, v_scale fp32 [pages][kv_heads]; a code stands for code * scale of its page and head, scales >= 0.
  * page_tokens 32, 64, 128 or 256; head_dim 64 or 128 (E_SHAPE otherwise).  Neither has to be initialised. */
 typedef enum { STRAIT_KV_F16 = 0, STRAIT_KV_I8 = 1 } strait_kv_type;
 typedef struct strait_kv_cache {

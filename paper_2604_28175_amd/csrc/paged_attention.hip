@@ -140,8 +140,10 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_stream_kernel(const
     }
     const float c = p.scale * 1.44269504088896340736f * (I8 ? 512.f : 1.f);
 
-    auto work = [&](const RawBlock<D, I8>& raw, int k0, float kc, float vs, auto masked) __attribute__((always_inline)) {
-        constexpr bool MASK = decltype(masked)::value;
+    // whether a row sees the key `off` behind some key of which it is `past` tokens past and which is `sinks` keys in front of the last sink
+    const int window = p.window ? p.window : 0x7fffffff;
+    auto sees = [&](int off, int past, int sinks) __attribute__((always_inline)) { return off <= past && (off > past - window || off < sinks); };
+    auto work = [&](const RawBlock<D, I8>& raw, int k0, float kc, float vs, bool mask) __attribute__((always_inline)) {
         half8 kf[2][D / 32];
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
@@ -169,9 +171,8 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_stream_kernel(const
                 for (int u = 0; u < D / 32; ++u) d = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[kb][u], qf[x][u], d, 0, 0, 0);
 #pragma unroll
                 for (int v = 0; v < 4; ++v) {
-                    const int key = k0 + 16 * kb + 4 * g4 + v;
                     sc[4 * kb + v] = d[v] * kc;
-                    if (MASK && !(key <= pos[x] && (!p.window || pos[x] - key < p.window || key < p.sinks))) sc[4 * kb + v] = -INFINITY;
+                    if (mask && !sees(16 * kb + v, pos[x] - k0 - 4 * g4, p.sinks - k0 - 4 * g4)) sc[4 * kb + v] = -INFINITY;
                     top = fmaxf(top, sc[4 * kb + v]);
                 }
             }
@@ -197,7 +198,7 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_stream_kernel(const
         for (int e = 0; e < 8; ++e) {
             // (a value that no row sees may be anything: 0 times an infinity is none of its business)
             const int key = k0 + 16 * (e >> 2) + 4 * g4 + (e & 3);
-            const bool seen = !MASK || I8 || (key <= t.hi && (!p.window || t.lo - key < p.window || key < p.sinks));
+            const bool seen = !mask || I8 || (key <= t.hi && (!p.window || t.lo - key < p.window || key < p.sinks));
 #pragma unroll
             for (int u = 0; u < RawBlock<D, I8>::VW; ++u) w[e][u] = I8 ? raw.v[e][u] ^ 0x80808080u : seen ? raw.v[e][u] : 0u;
         }
@@ -255,8 +256,7 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_stream_kernel(const
             const int k0 = __builtin_amdgcn_readlane(k0s, i);
             const float kc = I8 ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, kcs), i)) : c;
             const float vs = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, vss), i));
-            if (k0 + KEYS - 1 <= t.lo && (!p.window || t.hi - k0 < p.window || k0 + KEYS - 1 < p.sinks)) work(raw, k0, kc, vs, std::false_type{});
-            else work(raw, k0, kc, vs, std::true_type{});
+            work(raw, k0, kc, vs, !(k0 + KEYS - 1 <= t.lo && (!p.window || t.hi - k0 < p.window || k0 + KEYS - 1 < p.sinks)));
         }
     }
 #pragma unroll
@@ -400,7 +400,7 @@ __global__ void __launch_bounds__(64 * NW, 2) paged_tile_kernel(const PagedArgs 
                 k0s = k0;
                 places = page * H + h;
                 if (I8) {
-                    kcs = p.cache.k_scale[places] * c;
+                    kcs = fmaxf(p.cache.k_scale[places], 0x1p-100f) * c;       // (a scale of 0 belongs to codes of 0; times it, minus infinity were none)
                     // a value is code 2^(f - 9), exact in fp16, f between -15 and 15; the rest of its scale goes into the probabilities
                     const float vs = p.cache.v_scale[places] * 512.f;
                     vpow = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, vs) & 0x7f800000u);
@@ -458,11 +458,19 @@ __global__ void __launch_bounds__(64 * NW, 2) paged_tile_kernel(const PagedArgs 
         vaddr[db] = lds0 + TILE_KEYS * ROW + vr * ROW + (((db * 4 + ((lane >> 4) & 1) * 2 + ((i16 & 3) >> 1)) ^ vswz(vr)) << 4) + (i16 & 1) * 8;
     auto vread = [](unsigned at) { return __builtin_amdgcn_ds_read_tr16_b64_v4f16((__attribute__((address_space(3))) fp16x4*)(uintptr_t)at); };
 
-    auto work = [&](int n, int st, auto masked) __attribute__((always_inline)) {
-        constexpr bool MASK = decltype(masked)::value;
+    // whether a row sees the key `off` behind some key of which it is `past` tokens past and which is `sinks` keys in front of the last sink
+    const int window = p.window ? p.window : 0x7fffffff;
+    auto sees = [&](int off, int past, int sinks) __attribute__((always_inline)) { return off <= past && (off > past - window || off < sinks); };
+    auto work = [&](int n, int st, bool mask) __attribute__((always_inline)) {
         const char* ks0 = tile_lds + st * STAGE;
         floatx16 sc[2];                                // lane holds its row against keys 32 kb + 8 g + 4 lh + j of the tile (v = 4 g + j)
         float kc[2], top = -INFINITY;
+        half8 kf[D / 16];
+        auto read_key = [&](int kb, int ks) __attribute__((always_inline)) { kf[ks] = *(const half8*)(ks0 + (kb * 32 + l32) * ROW + (((ks * 2 + lh) ^ kswz(l32)) << 4)); };
+        // (the barriers keep the scheduler from holding more operands than there are registers for)
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) read_key(0, ks);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
             kc[kb] = I8 ? of_blockf(kcs, n + kb) : c;
@@ -470,22 +478,20 @@ __global__ void __launch_bounds__(64 * NW, 2) paged_tile_kernel(const PagedArgs 
 #pragma unroll
             for (int v = 0; v < 16; ++v) sc[kb][v] = 0.f;
 #pragma unroll
-            for (int ks = 0; ks < D / 16; ++ks)
-                sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const half8*)(ks0 + (kb * 32 + l32) * ROW + (((ks * 2 + lh) ^ kswz(l32)) << 4)), qf[ks], sc[kb], 0, 0, 0);
-            if (MASK) {
-#pragma unroll
-                for (int v = 0; v < 16; ++v) {
-                    const int key = k0 + 8 * (v >> 2) + 4 * lh + (v & 3);
-                    sc[kb][v] = key <= pos && (!p.window || pos - key < p.window || key < p.sinks) ? sc[kb][v] * kc[kb] : -INFINITY;
-                    top = fmaxf(top, sc[kb][v]);
-                }
-                kc[kb] = 1.f;
-            } else {
-                float most = sc[kb][0];
-#pragma unroll
-                for (int v = 1; v < 16; ++v) most = fmaxf(most, sc[kb][v]);
-                top = fmaxf(top, most * kc[kb]);       // (scales are not negative)
+            for (int ks = 0; ks < D / 16; ++ks) {
+                sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[ks], qf[ks], sc[kb], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+                if (kb == 0) read_key(1, ks);
             }
+            __builtin_amdgcn_sched_barrier(0);
+            if (mask) {
+#pragma unroll
+                for (int v = 0; v < 16; ++v) sc[kb][v] = sees(8 * (v >> 2) + (v & 3), pos - k0 - 4 * lh, p.sinks - k0 - 4 * lh) ? sc[kb][v] : -INFINITY;
+            }
+            float most = sc[kb][0];
+#pragma unroll
+            for (int v = 1; v < 16; ++v) most = fmaxf(most, sc[kb][v]);
+            top = fmaxf(top, most * kc[kb]);
         }
         if (__any(top > m + 8.f)) {
             const float2 both = halves_of(top);
@@ -504,7 +510,14 @@ __global__ void __launch_bounds__(64 * NW, 2) paged_tile_kernel(const PagedArgs 
             float sum = 0.f;
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                half8 pf;
+                half8 pf, vf[D / 32];
+#pragma unroll
+                for (int db = 0; db < D / 32; ++db) {
+                    const unsigned at = vaddr[db] + (unsigned)(st * STAGE + (kb * 32 + half * 16) * ROW);
+                    const fp16x4 lo4 = vread(at), hi4 = vread(at + 8 * ROW);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) { vf[db][j] = (half_t)lo4[j]; vf[db][4 + j] = (half_t)hi4[j]; }
+                }
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     const float pv = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[kb][8 * half + j], kc[kb], off));
@@ -512,14 +525,8 @@ __global__ void __launch_bounds__(64 * NW, 2) paged_tile_kernel(const PagedArgs 
                     pf[j] = (half_t)pv;
                 }
 #pragma unroll
-                for (int db = 0; db < D / 32; ++db) {
-                    const unsigned at = vaddr[db] + (unsigned)(st * STAGE + (kb * 32 + half * 16) * ROW);
-                    const fp16x4 lo4 = vread(at), hi4 = vread(at + 8 * ROW);
-                    half8 vf;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) { vf[j] = (half_t)lo4[j]; vf[4 + j] = (half_t)hi4[j]; }
-                    o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pf, o[db], 0, 0, 0);
-                }
+                for (int db = 0; db < D / 32; ++db) o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[db], pf, o[db], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
             }
             l = I8 ? __builtin_fmaf(sum, of_blockf(vinv, n + kb), l) : l + sum;
         }
@@ -543,10 +550,7 @@ __global__ void __launch_bounds__(64 * NW, 2) paged_tile_kernel(const PagedArgs 
             // (a look-up replaces what the current tile still needs: it waits for the tile's end)
             const bool ahead = more && nn < 64;
             if (ahead) fetch(nn);
-            if (!skip) {
-                if (whole) work(n, st, std::false_type{});
-                else work(n, st, std::true_type{});
-            }
+            if (!skip) work(n, st, !whole);
             n = nn;
             first += 2;
             if (more) {
