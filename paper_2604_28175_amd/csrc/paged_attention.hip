@@ -63,7 +63,7 @@ struct PagedArgs {
     int group, tiles, rows;              // query heads of a kv head; tiles of a sequence's rows and head, rows of a tile
     int per_part, parts;                 // blocks of a part, parts at most
     float* o; float* ml;                 // of parts: [tokens heads][parts][D] and [..][2]: the output over the sum, the maximum and the sum
-    Divisor by_group, by_heads, by_seqs, by_tiles;
+    Divisor by_group, by_heads, by_seqs, by_tiles, by_q_heads, by_max_q;
 };
 
 // A tile's rows: of sequence s, lo .. hi the positions of the first and last one.
@@ -71,6 +71,18 @@ struct Tile { int r0, lo, hi; bool any; };
 __device__ __forceinline__ Tile tile_of(const PagedArgs& a, const Sequence& s, int tile) {
     const int r0 = tile * a.rows, last = divide(r0 + a.rows - 1, a.by_group);
     return {r0, s.past + divide(r0, a.by_group), s.past + (last < s.n ? last : s.n - 1), r0 < s.n * a.group};
+}
+
+// Workgroup ((part tiles + tile) seqs + b') heads + h: every sequence's first part comes before any second one, and a head stays on a chiplet where there are 8.  The
+// hardware deals workgroups out to the parts of a chiplet in turn and in order, one that is full holding up the others; so that no part of it gets the longest sequence
+// of every round, the sequences are moved on by one from round to round (chunks of four prompts: 0.56 -> 0.85 of the places busy).
+__device__ __forceinline__ void place_item(const PagedArgs& a, int item, int& h, int& b, int& part, int& tile) {
+    const int i1 = divide(item, a.by_heads), i2 = divide(i1, a.by_seqs);
+    h = item - i1 * a.p.cache.kv_heads;
+    b = i1 - i2 * a.p.batch.seqs + i2 - divide(i2, a.by_seqs) * a.p.batch.seqs;
+    if (b >= a.p.batch.seqs) b -= a.p.batch.seqs;
+    part = divide(i2, a.by_tiles);
+    tile = i2 - part * a.tiles;
 }
 
 // A block's bytes as they come from memory: keys 16 kb + l16 at 16-byte pieces of their dimensions, and the values of 8 keys at J dimensions.
@@ -106,9 +118,8 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_stream_kernel(const
     if (p.hp) __builtin_amdgcn_s_setprio(3);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l16 = lane & 15, g4 = lane >> 4;
     const int H = p.cache.kv_heads, P = p.cache.page_tokens;
-    // ((part tiles + tile) seqs + b) heads + h: every sequence's first part comes before any second one
-    const int i1 = divide((int)blockIdx.x, a.by_heads), h = (int)blockIdx.x - i1 * H, i2 = divide(i1, a.by_seqs), b = i1 - i2 * p.batch.seqs;
-    const int part = divide(i2, a.by_tiles), tile = i2 - part * a.tiles;
+    int h, b, part, tile;
+    place_item(a, (int)blockIdx.x, h, b, part, tile);
     const Sequence s = sequence(p.batch, b);
     const Tile t = tile_of(a, s, tile);
     if (!t.any) return;
@@ -172,10 +183,16 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_stream_kernel(const
 #pragma unroll
                 for (int v = 0; v < 4; ++v) {
                     sc[4 * kb + v] = d[v] * kc;
-                    if (mask && !sees(16 * kb + v, pos[x] - k0 - 4 * g4, p.sinks - k0 - 4 * g4)) sc[4 * kb + v] = -INFINITY;
-                    top = fmaxf(top, sc[4 * kb + v]);
                 }
             }
+            if (mask) {
+                asm volatile("");                      // (a branch: most blocks have nothing to mask)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (!sees(16 * (e >> 2) + (e & 3), pos[x] - k0 - 4 * g4, p.sinks - k0 - 4 * g4)) sc[e] = -INFINITY;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = fmaxf(top, sc[e]);
             if (__any(top > m[x] + 8.f)) {
                 top = fmaxf(top, __shfl_xor(top, 16));
                 top = fmaxf(top, __shfl_xor(top, 32));
@@ -345,18 +362,19 @@ __device__ __forceinline__ float2 halves_of(float v) {
 
 constexpr int TILE_KEYS = 64;            // two blocks
 
-template <int D, bool I8, int NW>
-__global__ void __launch_bounds__(64 * NW, 2) paged_tile_kernel(const PagedArgs a) {
-    constexpr int NT = 64 * NW, ROW = D * 2, STAGE = 2 * TILE_KEYS * ROW;      // bytes of a row of K or V in LDS, of a stage
+template <int D, bool I8>
+__global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const PagedArgs a) {
+    constexpr int NT = 64 * PAGED_WAVES, ROW = D * 2, STAGE = 2 * TILE_KEYS * ROW;      // bytes of a row of K or V in LDS, of a stage
     constexpr int ES = I8 ? 1 : 2, PER_ROW = D * ES / 16, HALF = TILE_KEYS * PER_ROW, NI = 2 * HALF / NT;   // 16-byte pieces in memory: of a row, of K; of a thread
-    static_assert(2 * HALF % NT == 0, "pieces");
+    static_assert(HALF % NT == 0, "pieces");
     extern __shared__ __attribute__((aligned(16))) char tile_lds[];    // two stages
     const PagedAttention& p = a.p;
     if (p.hp) __builtin_amdgcn_s_setprio(3);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, lh = lane >> 5;
     const int H = p.cache.kv_heads, P = p.cache.page_tokens;
-    const int i1 = divide((int)blockIdx.x, a.by_heads), h = (int)blockIdx.x - i1 * H, i2 = divide(i1, a.by_seqs), b = i1 - i2 * p.batch.seqs;
-    const int part = divide(i2, a.by_tiles), tile = a.tiles - 1 - (i2 - part * a.tiles);      // the last tiles see the most keys and go first
+    int h, b, part, tile;
+    place_item(a, (int)blockIdx.x, h, b, part, tile);
+    tile = a.tiles - 1 - tile;                         // the last tiles see the most keys and go first
     const Sequence s = sequence(p.batch, b);
     const Tile t = tile_of(a, s, tile);
     if (!t.any) return;
@@ -383,10 +401,10 @@ __global__ void __launch_bounds__(64 * NW, 2) paged_tile_kernel(const PagedArgs 
     float m = -INFINITY, l = 0.f;
     const float c = p.scale * 1.44269504088896340736f * (I8 ? 512.f : 1.f);
 
-    // ---- memory -> registers -> LDS.  Chunk q of 16 bytes of row r lies at q ^ (r % 16) for K (D = 64: r % 8), whose operand is 16 rows at one chunk, and at q ^ 2 (r % 4)
-    // (D = 64: q ^ the bits of r % 8 reversed) for V, whose operand is 4 rows at 2 chunks
+    // ---- memory -> registers -> LDS.  Chunk q of 16 bytes of row r lies at q ^ (r % 16) for K (D = 64: r % 8), whose operand is 16 rows at one chunk.  V's
+    // operand is 4 rows at 4 chunks at a time: the rows' bits go to the chunk's bits above those (and to the lowest, for the sake of the stores)
     auto kswz = [](int row) { return D == 128 ? row & 15 : row & 7; };
-    auto vswz = [](int row) { return D == 128 ? (row & 3) << 1 : ((row & 1) << 2) | (row & 2) | ((row >> 2) & 1); };
+    auto vswz = [](int row) { return D == 128 ? (row & 3) << 2 | (row & 1) : (row & 2) << 1; };
     uintx4 raw[NI];
     // a lane of each wavefront holds what is to be known of a block: where it begins, its place (-1: not seen), and its scales
     int k0s = 0, places = -1;
@@ -417,18 +435,22 @@ __global__ void __launch_bounds__(64 * NW, 2) paged_tile_kernel(const PagedArgs 
     auto fetch = [&](int n) __attribute__((always_inline)) {       // blocks n and n + 1 of the 64 that were looked up
 #pragma unroll
         for (int x = 0; x < NI; ++x) {
-            const int id = x * NT + tid, v = id >= HALF, rem = v ? id - HALF : id, row = rem / PER_ROW, piece = rem % PER_ROW;
-            const int blk = __builtin_amdgcn_readfirstlane(n + (row >> 5)), place = of_block(places, blk), k0 = of_block(k0s, blk), key = k0 + (row & 31);
-            // (what no row of the tile sees may be anything: it arrives as zeros)
-            const bool seen = place >= 0 && (I8 || (key <= t.hi && (!p.window || t.lo - key < p.window || key < p.sinks)));
+            const int v = x * NT >= HALF, rem = x * NT + tid - v * HALF, row = rem / PER_ROW;
+            const int blk = n + (PER_ROW * KEYS >= NT ? x * NT % HALF / (PER_ROW * KEYS) : __builtin_amdgcn_readfirstlane(row >> 5));
+            const int place = of_block(places, blk), k0 = of_block(k0s, blk);
             raw[x] = uintx4{0, 0, 0, 0};
-            if (seen) raw[x] = *(const uintx4*)((const char*)(v ? p.cache.v : p.cache.k) + ((long long)place * P + (k0 & (P - 1))) * (D * ES) + (unsigned)((row & 31) * PER_ROW + piece) * 16u);
+            if (place < 0) continue;
+            const char* from = (const char*)(v ? p.cache.v : p.cache.k) + ((long long)place * P + (k0 & (P - 1))) * (D * ES);
+            const uintx4 got = *(const uintx4*)(from + (unsigned)(rem & (KEYS * PER_ROW - 1)) * 16u);
+            // (what no row of the tile sees may be anything: of fp16 it becomes zeros)
+            const int key = k0 + (row & 31);
+            raw[x] = I8 || (key <= t.hi && (!p.window || t.lo - key < p.window || key < p.sinks)) ? got : uintx4{0, 0, 0, 0};
         }
     };
     auto stage = [&](int n, int st) __attribute__((always_inline)) {
 #pragma unroll
         for (int x = 0; x < NI; ++x) {
-            const int id = x * NT + tid, v = id >= HALF, rem = v ? id - HALF : id, row = rem / PER_ROW, piece = rem % PER_ROW;
+            const int v = x * NT >= HALF, rem = x * NT + tid - v * HALF, row = rem / PER_ROW, piece = rem % PER_ROW;
             char* dst = tile_lds + st * STAGE + v * (TILE_KEYS * ROW) + row * ROW;
             const int swz = v ? vswz(row) : kswz(row);
             if constexpr (I8) {
@@ -485,6 +507,7 @@ __global__ void __launch_bounds__(64 * NW, 2) paged_tile_kernel(const PagedArgs 
             }
             __builtin_amdgcn_sched_barrier(0);
             if (mask) {
+                asm volatile("");                      // (a branch: most blocks have nothing to mask)
 #pragma unroll
                 for (int v = 0; v < 16; ++v) sc[kb][v] = sees(8 * (v >> 2) + (v & 3), pos - k0 - 4 * lh, p.sinks - k0 - 4 * lh) ? sc[kb][v] : -INFINITY;
             }
@@ -518,6 +541,7 @@ __global__ void __launch_bounds__(64 * NW, 2) paged_tile_kernel(const PagedArgs 
 #pragma unroll
                     for (int j = 0; j < 4; ++j) { vf[db][j] = (half_t)lo4[j]; vf[db][4 + j] = (half_t)hi4[j]; }
                 }
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     const float pv = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[kb][8 * half + j], kc[kb], off));
@@ -596,15 +620,15 @@ __global__ void __launch_bounds__(64 * NW, 2) paged_tile_kernel(const PagedArgs 
     }
 }
 
-// Joins the parts of rows that were shared out: a wavefront per (token, head).
+// Joins the parts of rows that were shared out: a workgroup per (token, head), whose threads take 4 dimensions each and every few parts.
 template <int D>
 __global__ void __launch_bounds__(256) paged_join_kernel(const PagedArgs a) {
+    constexpr int GROUP = D / 4, GROUPS = 256 / GROUP;
+    __shared__ floatx4 sums[GROUPS][GROUP];
     const PagedAttention& p = a.p;
     if (p.hp) __builtin_amdgcn_s_setprio(3);
     const int lane = threadIdx.x & 63;
-    const int item = __builtin_amdgcn_readfirstlane((int)blockIdx.x * 4 + ((int)threadIdx.x >> 6));
-    const int hq = item % p.heads, bi = item / p.heads, i = bi % p.batch.max_q, b = bi / p.batch.max_q;
-    if (b >= p.batch.seqs) return;
+    const int bi = divide((int)blockIdx.x, a.by_q_heads), hq = (int)blockIdx.x - bi * p.heads, b = divide(bi, a.by_max_q), i = bi - b * p.batch.max_q;
     const Sequence s = sequence(p.batch, b);
     if (i >= s.n) return;
     const int g = hq - divide(hq, a.by_group) * a.group;
@@ -614,40 +638,53 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const PagedArgs a) {
     if (parts <= 1) return;
     const long long row = (long long)(s.first + i) * p.heads + hq;
     const float2* ml = (const float2*)a.ml + row * a.parts;
-    const float* o = a.o + row * a.parts * D + lane * (D / 64);
-    float top = -INFINITY;
+    const int group = (int)threadIdx.x / GROUP, d = (int)threadIdx.x % GROUP;
+    const floatx4* o = (const floatx4*)(a.o + row * a.parts * D) + d;
+    // (every wavefront finds the maximum and the sum for itself)
+    float top = -INFINITY, sum = 0.f;
     for (int x = lane; x < parts; x += 64) top = fmaxf(top, ml[x].x);
 #pragma unroll
-    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-    float sum = 0.f, y[D / 64] = {};
-    for (int x0 = 0; x0 < parts; x0 += 64) {
-        const float2 v = x0 + lane < parts ? ml[x0 + lane] : make_float2(-INFINITY, 0.f);
-        const float mine = v.y == 0.f ? 0.f : v.y * __builtin_amdgcn_exp2f(v.x - top);     // (NaN stays NaN)
-        sum += mine;
-        const int n = parts - x0 < 64 ? parts - x0 : 64;
-        for (int x = 0; x < n; ++x) {
-            const float w = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, mine), x));
+    for (int k = 32; k; k >>= 1) top = fmaxf(top, __shfl_xor(top, k));
+    auto weight = [&](float2 v) { return v.y == 0.f ? 0.f : v.y * __builtin_amdgcn_exp2f(v.x - top); };    // (NaN stays NaN)
+    for (int x = lane; x < parts; x += 64) sum += weight(ml[x]);
 #pragma unroll
-            for (int j = 0; j < D / 64; ++j) y[j] = __builtin_fmaf(w, o[(long long)(x0 + x) * D + j], y[j]);
+    for (int k = 32; k; k >>= 1) sum += __shfl_xor(sum, k);
+    floatx4 y = {0.f, 0.f, 0.f, 0.f};
+    for (int x = group; x < parts; x += 4 * GROUPS) {
+        floatx4 part[4];
+        float w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int at = x + k * GROUPS;
+            part[k] = o[(long long)(at < parts ? at : x) * GROUP];
+            w[k] = at < parts ? weight(ml[at]) : 0.f;
         }
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (x + k * GROUPS < parts) y += part[k] * w[k];
     }
+    sums[group][d] = y;
+    __syncthreads();
+    if (group) return;
 #pragma unroll
-    for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+    for (int k = 1; k < GROUPS; ++k) y += sums[k][d];
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    half_t* out = p.out + row * D + lane * (D / 64);
+    half_t h[4];
 #pragma unroll
-    for (int j = 0; j < D / 64; ++j) out[j] = (half_t)(y[j] * inv);
+    for (int j = 0; j < 4; ++j) h[j] = (half_t)(y[j] * inv);
+    *(uint2*)(p.out + row * D + d * 4) = *(const uint2*)h;
 }
 
-// How a call is launched.  Up to 32 rows of a sequence and kv head: the stream kernel, tiles of 16 or 32 rows.  More: the tile kernel, 128 rows, or 256 where those
-// still give every compute unit one.  Parts of as many blocks as give each compute unit several workgroups (tile kernel: one).
+// How a call is launched.  Up to 32 rows of a sequence and kv head: the stream kernel, tiles of 16 or 32 rows.  More: the tile kernel, 128 rows, of
+// which a compute unit holds two.  (256 rows by eight wavefronts fill LDS half as often, but all of them stand at one barrier: chunks of four prompts 274 and 274 us, with a
+// window 74 and 97.)  Parts of as many blocks as give each compute unit several workgroups (tile kernel: one).
 static PagedArgs paged_plan(const PagedAttention& p) {
     PagedArgs a{};
     a.p = p;
     a.group = p.heads / p.cache.kv_heads;
     const long long rows = (long long)p.batch.max_q * a.group, pairs = (long long)p.batch.seqs * p.cache.kv_heads;
     const bool stream = rows <= 32;
-    a.rows = rows <= 16 ? 16 : stream ? 32 : pairs * ((rows + 255) / 256) >= 256 ? 256 : 128;
+    a.rows = rows <= 16 ? 16 : stream ? 32 : 128;
     a.tiles = (int)((rows + a.rows - 1) / a.rows);
     const int most = most_blocks(p, a.rows);
     const long long work = pairs * a.tiles * most;
@@ -655,7 +692,7 @@ static PagedArgs paged_plan(const PagedAttention& p) {
     a.per_part = (int)std::min<long long>(most, std::max<long long>(stream ? 8 : 16, (per + PAGED_WAVES - 1) / PAGED_WAVES * PAGED_WAVES));
     if (!stream && pairs * a.tiles >= 256) a.per_part = most;
     a.parts = (most + a.per_part - 1) / a.per_part;
-    a.by_group = divisor(a.group); a.by_heads = divisor(p.cache.kv_heads); a.by_seqs = divisor(p.batch.seqs); a.by_tiles = divisor(a.tiles);
+    a.by_group = divisor(a.group); a.by_heads = divisor(p.cache.kv_heads); a.by_seqs = divisor(p.batch.seqs); a.by_tiles = divisor(a.tiles); a.by_q_heads = divisor(p.heads); a.by_max_q = divisor(p.batch.max_q);
     a.ml = p.ws;
     const size_t head = ((size_t)p.batch.tokens * p.heads * a.parts * 2 * sizeof(float) + 15) / 16 * 16;
     a.o = (float*)((char*)p.ws + head);
@@ -677,15 +714,14 @@ static void launch_paged(const PagedArgs& a, unsigned grid, hipStream_t stream) 
     } else {
         constexpr unsigned lds = 2 * 2 * TILE_KEYS * D * 2;
         static_assert(lds <= 64 * 1024, "what a kernel may have unasked");
-        if (a.rows == 256) hipLaunchKernelGGL((paged_tile_kernel<D, I8, 8>), dim3(grid), dim3(512), lds, stream, a);
-        else hipLaunchKernelGGL((paged_tile_kernel<D, I8, 4>), dim3(grid), dim3(256), lds, stream, a);
+        hipLaunchKernelGGL((paged_tile_kernel<D, I8>), dim3(grid), dim3(64 * PAGED_WAVES), lds, stream, a);
     }
 }
 
 int launch_paged_attention(const PagedAttention& p, hipStream_t stream) {
     const PagedArgs a = paged_plan(p);
-    const long long grid = (long long)p.batch.seqs * p.cache.kv_heads * a.tiles * a.parts, joins = ((long long)p.batch.seqs * p.batch.max_q * p.heads + 3) / 4;
-    if (grid > 0x7fffffffLL || joins > 0x1fffffffLL) { set_error("attention_paged: grid too large"); return STRAIT_E_SHAPE; }
+    const long long grid = (long long)p.batch.seqs * p.cache.kv_heads * a.tiles * a.parts, joins = (long long)p.batch.seqs * p.batch.max_q * p.heads;
+    if (grid > 0x7fffffffLL || (a.parts > 1 && joins > 0x7fffffffLL)) { set_error("attention_paged: grid too large"); return STRAIT_E_SHAPE; }
     const bool i8 = p.cache.type == STRAIT_KV_I8;
     if (p.cache.head_dim == 64) i8 ? launch_paged<64, true>(a, (unsigned)grid, stream) : launch_paged<64, false>(a, (unsigned)grid, stream);
     else i8 ? launch_paged<128, true>(a, (unsigned)grid, stream) : launch_paged<128, false>(a, (unsigned)grid, stream);
