@@ -20,6 +20,10 @@ namespace strait {
 
 typedef int intx16 __attribute__((ext_vector_type(16)));
 
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+struct __attribute__((packed, aligned(2))) AnyHalf8 { half8 h; };      // at any address of an element
+struct __attribute__((packed, aligned(4))) AnyFloat4 { floatx4 f; };
+
 // One output of a sum: the same operations in the same order in every kernel, so that a row has the same bits whatever launch it is part of.
 __device__ __forceinline__ float finish(int sum, float xs, float ws, float bias, float res, int act) {
     return apply_act(__builtin_fmaf((float)sum, xs * ws, bias) + res, act);
@@ -27,11 +31,11 @@ __device__ __forceinline__ float finish(int sum, float xs, float ws, float bias,
 
 // ---- few rows -------------------------------------------------------------------------------------------------------
 
-constexpr int STREAM_WAVES = 8, STREAM_STEPS = 4;      // steps of 64 in a piece
+constexpr int STREAM_WAVES = 8;
 
-template <int MT, int NT>
+template <int MT, int NT, int STREAM_STEPS>
 __global__ void __launch_bounds__(64 * STREAM_WAVES) gemm_i8_stream_kernel(const GemmI8 p) {
-    __shared__ int sums[16 * MT][16 * NT];
+    __shared__ int sums[16 * MT][16 * NT + 1];          // (+ 1: 16 rows at one channel lie in 16 banks)
     if (p.hp) __builtin_amdgcn_s_setprio(3);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l16 = lane & 15, g4 = lane >> 4;
     const int n0 = (int)blockIdx.x * 16 * NT, m0 = (int)blockIdx.y * 16 * MT;
@@ -60,7 +64,7 @@ __global__ void __launch_bounds__(64 * STREAM_WAVES) gemm_i8_stream_kernel(const
             for (int s = 0; s < STREAM_STEPS; ++s) x[t][s] = at(xr[t], piece, s);
     };
     if (wave < pieces) load(wave);
-    for (int i = threadIdx.x; i < 256 * MT * NT; i += 64 * STREAM_WAVES) (&sums[0][0])[i] = 0;
+    for (int i = threadIdx.x; i < 16 * MT * (16 * NT + 1); i += 64 * STREAM_WAVES) (&sums[0][0])[i] = 0;
     for (int piece = wave; piece < pieces; piece += STREAM_WAVES) {
         intx4 wc[NT][STREAM_STEPS], xc[MT][STREAM_STEPS];
 #pragma unroll
@@ -191,42 +195,109 @@ __global__ void __launch_bounds__(64 * WGM * WGN, (tile_waves_per_simd<BM, BN, W
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");   // the zeros past the end have arrived: LDS is free
 
-    // ---- epilogue: a lane holds y[m][n .. n + 3] of 8 g + 4 lh; fp16 results leave through LDS, 16 bytes a lane
-    half_t* const out = (half_t*)tile_smem;
+    // ---- epilogue: a lane holds the sums of y[m][n .. n + 3], n at 8 g + 4 lh.  Rows of the result begin at any multiple of its element (N may be odd): 16 bytes at a time
+    // all the same, which the memory takes at any address.
+    if (!p.out_f32 && !p.res) {
+        // rounded results leave through LDS
+        half_t* const out = (half_t*)tile_smem;
+#pragma unroll
+        for (int b = 0; b < TMB; ++b) {
+            const int mt = wm0 + b * 32 + l32;
+            const float xs = m0 + mt < p.M ? p.xs[m0 + mt] : 0.f;
+#pragma unroll
+            for (int t = 0; t < TNB; ++t)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const int nt = wn0 + t * 32 + 8 * g + 4 * lh;
+                    half4 h;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int n = n0 + nt + j < p.N ? n0 + nt + j : p.N - 1;
+                        h[j] = (half_t)finish(acc[t][b][4 * g + j], xs, p.ws[n], p.bias ? p.bias[n] : 0.f, 0.f, p.act);
+                    }
+                    *(half4*)(out + mt * LDC + nt) = h;
+                }
+        }
+        __syncthreads();
+        for (int i = tid; i < BM * (BN / 8); i += NT) {
+            const int r = i / (BN / 8), c = (i - r * (BN / 8)) * 8, m = m0 + r, n = n0 + c;
+            if (m >= p.M || n >= p.N) continue;
+            half_t* y = (half_t*)p.y + (long long)m * p.N + n;
+            const half8 h = *(const half8*)(out + r * LDC + c);
+            if (n + 8 <= p.N) *(AnyHalf8*)y = AnyHalf8{h};
+            else
+                for (int j = 0; j < p.N - n; ++j) y[j] = out[r * LDC + c + j];
+        }
+        return;
+    }
+    // with a residual, or in fp32: the sums go through LDS, 32 rows of each wavefront at a time, and are finished by lanes that lie along a row, 8 outputs each
+    int* const sums = (int*)tile_smem;
+    constexpr int LDS_N = BN + 4, LANES = BN / 8, ROWS = WGM * 32 / (NT / LANES);     // lanes along a row, rows of a lane
+    static_assert(WGM * 32 * LDS_N * 4 <= (int)tile_lds<BM, BN, WGM, WGN, STAGES>() && WGM * 32 % (NT / LANES) == 0, "staging");
+    const int c0 = tid % LANES * 8, n = n0 + c0, many = p.N - n < 8 ? p.N - n : 8;
+    float ws[8], bias[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int c = n + j < p.N ? n + j : p.N - 1;
+        ws[j] = p.ws[c];
+        bias[j] = p.bias ? p.bias[c] : 0.f;
+    }
 #pragma unroll
     for (int b = 0; b < TMB; ++b) {
-        const int mt = wm0 + b * 32 + l32, m = m0 + mt;
-        const float xs = m < p.M ? p.xs[m] : 0.f;
-        const long long row = (long long)m * p.N;
+        // (the residual is on its way while the sums are)
+        half8 res[ROWS];
+        float xs[ROWS];
+        int ms[ROWS];
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+            const int r = i * (NT / LANES) + tid / LANES;
+            const int m = ms[i] = m0 + r / 32 * TM + b * 32 + r % 32;
+            xs[i] = m < p.M ? p.xs[m] : 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) res[i][j] = (half_t)0.f;
+            if (p.res && m < p.M) {
+                const half_t* at = p.res + (long long)m * p.N + n;
+                if (many == 8) res[i] = ((const AnyHalf8*)at)->h;
+                else
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (j < many) res[i][j] = at[j];
+            }
+        }
+        if (b) __syncthreads();
 #pragma unroll
         for (int t = 0; t < TNB; ++t)
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int nt = wn0 + t * 32 + 8 * g + 4 * lh, n = n0 + nt;
-                half4 h;
+            for (int g = 0; g < 4; ++g)
+                *(intx4*)(sums + ((wave % WGM) * 32 + l32) * LDS_N + wn0 + t * 32 + 8 * g + 4 * lh) = intx4{acc[t][b][4 * g], acc[t][b][4 * g + 1], acc[t][b][4 * g + 2], acc[t][b][4 * g + 3]};
+        __syncthreads();
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const bool real = m < p.M && n + j < p.N;
-                    const int c = n + j < p.N ? n + j : p.N - 1;
-                    const float y = finish(acc[t][b][4 * g + j], xs, p.ws[c], p.bias ? p.bias[c] : 0.f, p.res && real ? (float)p.res[row + n + j] : 0.f, p.act);
-                    if (p.out_f32) {
-                        if (real) ((float*)p.y)[row + n + j] = y;
-                    } else h[j] = (half_t)y;
-                }
-                if (!p.out_f32) *(half4*)(out + mt * LDC + nt) = h;
+        for (int i = 0; i < ROWS; ++i) {
+            const int* from = sums + (i * (NT / LANES) + tid / LANES) * LDS_N + c0;
+            const intx4 lo = *(const intx4*)from, hi = *(const intx4*)(from + 4);
+            float y[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = finish(j < 4 ? lo[j] : hi[j - 4], xs[i], ws[j], bias[j], (float)res[i][j], p.act);
+            if (ms[i] >= p.M || many <= 0) continue;
+            const long long at = (long long)ms[i] * p.N + n;
+            if (p.out_f32) {
+                if (many == 8) {
+                    *(AnyFloat4*)((float*)p.y + at) = AnyFloat4{floatx4{y[0], y[1], y[2], y[3]}};
+                    *(AnyFloat4*)((float*)p.y + at + 4) = AnyFloat4{floatx4{y[4], y[5], y[6], y[7]}};
+                } else
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (j < many) ((float*)p.y)[at + j] = y[j];
+            } else {
+                half8 h;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) h[j] = (half_t)y[j];
+                if (many == 8) *(AnyHalf8*)((half_t*)p.y + at) = AnyHalf8{h};
+                else
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (j < many) ((half_t*)p.y)[at + j] = h[j];
             }
-    }
-    if (p.out_f32) return;
-    __syncthreads();
-    if (p.N % 8 == 0 && (reinterpret_cast<uintptr_t>(p.y) & 15) == 0) {
-        for (int i = tid; i < BM * (BN / 8); i += NT) {
-            const int r = i / (BN / 8), c = (i - r * (BN / 8)) * 8;
-            if (m0 + r < p.M && n0 + c < p.N) *(half8*)((half_t*)p.y + (long long)(m0 + r) * p.N + n0 + c) = *(const half8*)(out + r * LDC + c);
-        }
-    } else {
-        for (int i = tid; i < BM * BN; i += NT) {
-            const int r = i / BN, c = i - r * BN;
-            if (m0 + r < p.M && n0 + c < p.N) ((half_t*)p.y)[(long long)(m0 + r) * p.N + n0 + c] = out[r * LDC + c];
         }
     }
 }
@@ -249,21 +320,18 @@ static int launch_tile(const GemmI8& p, hipStream_t stream) {
     hipLaunchKernelGGL(kernel, dim3((unsigned)(tiles_m * tiles_n)), dim3(64 * WGM * WGN), lds, stream, a);
     return 0;
 }
-template <int MT, int NT>
+template <int MT, int NT, int STEPS>
 static void launch_stream(const GemmI8& p, hipStream_t stream) {
-    hipLaunchKernelGGL((gemm_i8_stream_kernel<MT, NT>), dim3((unsigned)((p.N + 16LL * NT - 1) / (16 * NT)), (unsigned)((p.M + 16 * MT - 1) / (16 * MT))), dim3(64 * STREAM_WAVES), 0, stream, p);
+    hipLaunchKernelGGL((gemm_i8_stream_kernel<MT, NT, STEPS>), dim3((unsigned)((p.N + 16LL * NT - 1) / (16 * NT)), (unsigned)((p.M + 16 * MT - 1) / (16 * MT))), dim3(64 * STREAM_WAVES), 0, stream, p);
 }
 
 int launch_gemm_i8(const GemmI8& p, hipStream_t stream) {
     int rc = 0;
     if (p.M <= 64) {
         const int mt = (p.M + 15) / 16, nt = p.N >= 16384 ? 4 : p.N >= 8192 ? 2 : 1;
-#define STRAIT_GO(MT) (nt == 4 ? launch_stream<MT, 4>(p, stream) : nt == 2 ? launch_stream<MT, 2>(p, stream) : launch_stream<MT, 1>(p, stream))
-        if (mt == 1) STRAIT_GO(1);
-        else if (mt == 2) STRAIT_GO(2);
-        else if (mt == 3) STRAIT_GO(3);
-        else STRAIT_GO(4);
-#undef STRAIT_GO
+        if (mt == 1) nt == 4 ? launch_stream<1, 4, 2>(p, stream) : nt == 2 ? launch_stream<1, 2, 4>(p, stream) : launch_stream<1, 1, 4>(p, stream);
+        else if (mt == 2) nt == 4 ? launch_stream<2, 4, 2>(p, stream) : nt == 2 ? launch_stream<2, 2, 4>(p, stream) : launch_stream<2, 1, 4>(p, stream);
+        else nt == 4 ? launch_stream<4, 4, 2>(p, stream) : nt == 2 ? launch_stream<4, 2, 2>(p, stream) : launch_stream<4, 1, 2>(p, stream);
     } else if ((p.M + 255LL) / 256 * ((p.N + 255LL) / 256) >= 256) rc = launch_tile<256, 256, 2, 4, 4>(p, stream);
     else rc = launch_tile<128, 128, 2, 2, 4>(p, stream);
     if (rc) return rc;
