@@ -8,7 +8,7 @@
 //   out in pieces of 256; weights go from memory to registers in the layout of v_mfma_i32_16x16x64_i8's operand, a piece ahead, and each byte is read
 //   once on the whole chip.  The partial sums meet in LDS as integers.
 //
-//   gemm_i8_tile_kernel: bound by the matrix pipes.  Slices of 64 of the reduction travel to a ring in LDS without passing through registers, the operands of
+//   gemm_i8_tile_kernel: bound by the matrix pipes.  Slices of 128 of the reduction travel to a ring in LDS without passing through registers, the operands of
 //   the next MFMAs are read while the current ones run, and one barrier per slice hands a stage on.
 #include <type_traits>
 
@@ -107,9 +107,10 @@ __global__ void __launch_bounds__(64 * STREAM_WAVES) gemm_i8_stream_kernel(const
 
 struct TileArgs { GemmI8 g; TileOrder order; };
 
+constexpr int SLICE = 128;               // of the reduction, a whole cache line of each row
 template <int BM, int BN, int WGM, int WGN, int STAGES>
 constexpr unsigned tile_lds() {
-    const unsigned ring = STAGES * (BM + BN) * 64, out = BM * (BN + 8) * 2;
+    const unsigned ring = STAGES * (BM + BN) * SLICE, out = BM * (BN + 8) * 2;
     return ring > out ? ring : out;
 }
 template <int BM, int BN, int WGM, int WGN, int STAGES>
@@ -122,11 +123,11 @@ template <int BM, int BN, int WGM, int WGN, int STAGES>
 __global__ void __launch_bounds__(64 * WGM * WGN, (tile_waves_per_simd<BM, BN, WGM, WGN, STAGES>())) gemm_i8_tile_kernel(const TileArgs a) {
     const GemmI8& p = a.g;
     constexpr int NW = WGM * WGN, NT = 64 * NW;
-    constexpr int TM = BM / WGM, TN = BN / WGN, TMB = TM / 32, TNB = TN / 32;
-    constexpr int XI = BM / (16 * NW), WI = BN / (16 * NW), NX = XI + WI, NM = TMB * TNB;    // transfers of 16 rows per wavefront and slice; MFMAs per step
-    constexpr unsigned STAGE = (BM + BN) * 64;
+    constexpr int TM = BM / WGM, TN = BN / WGN, TMB = TM / 32, TNB = TN / 32, KS = SLICE / 32;
+    constexpr int XI = BM / (8 * NW), WI = BN / (8 * NW), NX = XI + WI, NM = TMB * TNB;      // transfers of 8 rows per wavefront and slice; MFMAs per step
+    constexpr unsigned STAGE = (BM + BN) * SLICE;
     constexpr int LDC = BN + 8;
-    static_assert(TM % 32 == 0 && TN % 32 == 0 && BM % (16 * NW) == 0 && BN % (16 * NW) == 0 && STAGES >= 3 && tile_lds<BM, BN, WGM, WGN, STAGES>() <= 160 * 1024, "tile");
+    static_assert(TM % 32 == 0 && TN % 32 == 0 && BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && NW % 2 == 0 && STAGES >= 2 && tile_lds<BM, BN, WGM, WGN, STAGES>() <= 160 * 1024, "tile");
 
     extern __shared__ __attribute__((aligned(1024))) char tile_smem[];
     if (p.hp) __builtin_amdgcn_s_setprio(3);
@@ -140,58 +141,62 @@ __global__ void __launch_bounds__(64 * WGM * WGN, (tile_waves_per_simd<BM, BN, W
     // the tile's rows as buffers of their own: offsets stay below 256 * 131056 whatever the operands' size; rows and numbers past the end arrive as zeros
     const intx4 xrsrc = make_rsrc(p.x + (long long)m0 * p.K, (unsigned)(p.M - m0 < BM ? p.M - m0 : BM) * (unsigned)p.K);
     const intx4 wrsrc = make_rsrc(p.w + (long long)n0 * p.K, (unsigned)(p.N - n0 < BN ? p.N - n0 : BN) * (unsigned)p.K);
-    // lane i brings 16 bytes of row i / 4; LDS holds chunk c of a row r at c ^ (r / 4 % 4), so that 16 rows read at one chunk meet no bank twice
-    const int rsub = lane >> 2, cl = (lane & 3) ^ ((rsub >> 2) & 3);
+    // lane i brings 16 bytes of row i / 8; LDS holds chunk c of a row r at c ^ (r / 2 % 8), so that 16 rows read at one chunk meet no bank twice
+    const int rsub = lane >> 3, cl = (lane & 7) ^ (((wave * 8 + rsub) >> 1) & 7);
     unsigned xoff[XI], woff[WI];
 #pragma unroll
-    for (int j = 0; j < XI; ++j) xoff[j] = m0 + (j * NW + wave) * 16 + rsub < p.M ? (unsigned)((j * NW + wave) * 16 + rsub) * (unsigned)p.K + cl * 16 : OOB_OFFSET;
+    for (int j = 0; j < XI; ++j) xoff[j] = m0 + (j * NW + wave) * 8 + rsub < p.M ? (unsigned)((j * NW + wave) * 8 + rsub) * (unsigned)p.K + cl * 16 : OOB_OFFSET;
 #pragma unroll
-    for (int j = 0; j < WI; ++j) woff[j] = n0 + (j * NW + wave) * 16 + rsub < p.N ? (unsigned)((j * NW + wave) * 16 + rsub) * (unsigned)p.K + cl * 16 : OOB_OFFSET;
-    const int nk = (p.K + 63) / 64;
+    for (int j = 0; j < WI; ++j) woff[j] = n0 + (j * NW + wave) * 8 + rsub < p.N ? (unsigned)((j * NW + wave) * 8 + rsub) * (unsigned)p.K + cl * 16 : OOB_OFFSET;
+    const int nk = (p.K + SLICE - 1) / SLICE;
     auto issue_one = [&](int stage, int slice, int j) __attribute__((always_inline)) {
-        const bool there = slice * 64 + cl * 16 < p.K;             // (the last slice may be ragged)
+        const bool there = slice * SLICE + cl * 16 < p.K;          // (the last slice may be ragged)
         const unsigned at = lds0 + (unsigned)stage * STAGE;
-        if (j < XI) dma16(xrsrc, there ? xoff[j] : OOB_OFFSET, (unsigned)slice * 64u, at + (unsigned)((j * NW + wave) * 1024));
-        else dma16(wrsrc, there ? woff[j - XI] : OOB_OFFSET, (unsigned)slice * 64u, at + BM * 64u + (unsigned)(((j - XI) * NW + wave) * 1024));
+        if (j < XI) dma16(xrsrc, there ? xoff[j] : OOB_OFFSET, (unsigned)(slice * SLICE), at + (unsigned)((j * NW + wave) * 1024));
+        else dma16(wrsrc, there ? woff[j - XI] : OOB_OFFSET, (unsigned)(slice * SLICE), at + BM * SLICE + (unsigned)(((j - XI) * NW + wave) * 1024));
     };
     intx16 acc[TNB][TMB] = {};
     intx4 wf[2][TNB], xf[2][TMB];
     auto load_frags = [&](int buf, int stage, int ks) __attribute__((always_inline)) {
         const char* xs = tile_smem + stage * (int)STAGE;
-        const char* ws = xs + BM * 64;
-        const int pos = ((ks * 2 + lh) ^ ((l32 >> 2) & 3)) * 16;
+        const char* ws = xs + BM * SLICE;
+        const int pos = ((ks * 2 + lh) ^ ((l32 >> 1) & 7)) * 16;
 #pragma unroll
-        for (int i = 0; i < TNB; ++i) wf[buf][i] = *(const intx4*)(ws + (wn0 + i * 32 + l32) * 64 + pos);
+        for (int i = 0; i < TNB; ++i) wf[buf][i] = *(const intx4*)(ws + (wn0 + i * 32 + l32) * SLICE + pos);
 #pragma unroll
-        for (int i = 0; i < TMB; ++i) xf[buf][i] = *(const intx4*)(xs + (wm0 + i * 32 + l32) * 64 + pos);
+        for (int i = 0; i < TMB; ++i) xf[buf][i] = *(const intx4*)(xs + (wm0 + i * 32 + l32) * SLICE + pos);
     };
-    // STAGES - 1 slices under way; slices past the end are requested as zeros, so that every wait counts the same
+    // STAGES slices under way; slices past the end are requested as zeros, so that every wait counts the same
 #pragma unroll
-    for (int s = 0; s < STAGES - 1; ++s)
+    for (int s = 0; s < STAGES; ++s)
 #pragma unroll
         for (int j = 0; j < NX; ++j) issue_one(s, s, j);
-    wait_loads_then_barrier<(STAGES - 2) * NX>();
+    wait_loads_then_barrier<(STAGES - 1) * NX>();
     load_frags(0, 0, 0);
-    int rd = 0, fill = STAGES - 1;
+    int rd = 0;
     for (int kt = 0; kt < nk; ++kt) {
-        load_frags(1, rd, 1);
-        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int q = 0; q < NM; ++q) {
-            acc[q / TMB][q % TMB] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf[0][q / TMB], xf[0][q % TMB], acc[q / TMB][q % TMB], 0, 0, 0);
-            constexpr int PER = (NX + NM - 1) / NM;
+        for (int ks = 0; ks < KS; ++ks) {
+            const int left = rd;
+            if (ks + 1 < KS) load_frags((ks + 1) & 1, rd, ks + 1);
+            else {
+                wait_loads_then_barrier<(STAGES - 2) * NX>();      // slice kt + 1 is there, and everyone has read slice kt
+                rd = rd + 1 == STAGES ? 0 : rd + 1;
+                load_frags(0, rd, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int j = q * PER; j < (q + 1) * PER && j < NX; ++j) issue_one(fill, kt + STAGES - 1, j);
+            for (int q = 0; q < NM; ++q) {
+                acc[q / TMB][q % TMB] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf[ks & 1][q / TMB], xf[ks & 1][q % TMB], acc[q / TMB][q % TMB], 0, 0, 0);
+                if (ks == KS - 1) {
+                    constexpr int PER = (NX + NM - 1) / NM;
+#pragma unroll
+                    for (int j = q * PER; j < (q + 1) * PER && j < NX; ++j) issue_one(left, kt + STAGES, j);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
             __builtin_amdgcn_sched_barrier(0);
         }
-        wait_loads_then_barrier<(STAGES - 2) * NX>();          // slice kt + 1 is there, and everyone has read slice kt
-        fill = rd;
-        rd = rd + 1 == STAGES ? 0 : rd + 1;
-        load_frags(0, rd, 0);
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int q = 0; q < NM; ++q) acc[q / TMB][q % TMB] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf[1][q / TMB], xf[1][q % TMB], acc[q / TMB][q % TMB], 0, 0, 0);
-        __builtin_amdgcn_sched_barrier(0);
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");   // the zeros past the end have arrived: LDS is free
 
@@ -307,7 +312,7 @@ static int launch_tile(const GemmI8& p, hipStream_t stream) {
     const long long tiles_m = (p.M + BM - 1LL) / BM, tiles_n = (p.N + BN - 1LL) / BN;
     if (tiles_m * tiles_n > 0x3fffffffLL) { set_error("gemm_i8: grid too large"); return STRAIT_E_SHAPE; }
     ConvParams order{};
-    set_tile_order(order, tiles_m, (int)tiles_n, BM, BN, 64, 1);
+    set_tile_order(order, tiles_m, (int)tiles_n, BM, BN, SLICE, 1);
     const TileArgs a{p, order.order};
     constexpr unsigned lds = tile_lds<BM, BN, WGM, WGN, STAGES>();
     auto kernel = gemm_i8_tile_kernel<BM, BN, WGM, WGN, STAGES>;
@@ -325,15 +330,30 @@ static void launch_stream(const GemmI8& p, hipStream_t stream) {
     hipLaunchKernelGGL((gemm_i8_stream_kernel<MT, NT, STEPS>), dim3((unsigned)((p.N + 16LL * NT - 1) / (16 * NT)), (unsigned)((p.M + 16 * MT - 1) / (16 * MT))), dim3(64 * STREAM_WAVES), 0, stream, p);
 }
 
+// Up to 64 rows: 16 NT channels to a workgroup, NT so that there are 256 workgroups where the channels allow it (16384 x 4096 at 48 rows, NT = 4, 2, 1: 18.1, 22.6 and 39.6 us; 4096 x
+// 4096: 16.8, 12.5 and 11.7), pieces of 64, 128 or 256 as the registers allow.
+// More: the tile with the least time for the most tiles that a compute unit gets.  A slice of 128 takes a unit 0.25 us on a 64 x 64 tile, 0.70 on 128 x 128, 1.23 on 256 x 128
+// and 2.42 on 256 x 256 with all units at work (256 x 4096 x 4096 12.7, 20.4, 31.5 and 55.9 us; 2048 x 4096 x 4096 70, 51.6, 43.4 and 60.2; 8192 x 16384 x 4096 1205, 862, 683 and 623).
 int launch_gemm_i8(const GemmI8& p, hipStream_t stream) {
     int rc = 0;
     if (p.M <= 64) {
-        const int mt = (p.M + 15) / 16, nt = p.N >= 16384 ? 4 : p.N >= 8192 ? 2 : 1;
-        if (mt == 1) nt == 4 ? launch_stream<1, 4, 2>(p, stream) : nt == 2 ? launch_stream<1, 2, 4>(p, stream) : launch_stream<1, 1, 4>(p, stream);
-        else if (mt == 2) nt == 4 ? launch_stream<2, 4, 2>(p, stream) : nt == 2 ? launch_stream<2, 2, 4>(p, stream) : launch_stream<2, 1, 4>(p, stream);
-        else nt == 4 ? launch_stream<4, 4, 2>(p, stream) : nt == 2 ? launch_stream<4, 2, 2>(p, stream) : launch_stream<4, 1, 2>(p, stream);
-    } else if ((p.M + 255LL) / 256 * ((p.N + 255LL) / 256) >= 256) rc = launch_tile<256, 256, 2, 4, 4>(p, stream);
-    else rc = launch_tile<128, 128, 2, 2, 4>(p, stream);
+        const int nt = p.N >= 16384 ? 4 : p.N >= 8192 ? 2 : 1;
+        if (p.M <= 16) nt == 4 ? launch_stream<1, 4, 2>(p, stream) : nt == 2 ? launch_stream<1, 2, 4>(p, stream) : launch_stream<1, 1, 4>(p, stream);
+        else if (p.M <= 32) nt == 4 ? launch_stream<2, 4, 2>(p, stream) : nt == 2 ? launch_stream<2, 2, 2>(p, stream) : launch_stream<2, 1, 4>(p, stream);
+        else if (p.M <= 48) nt == 4 ? launch_stream<3, 4, 1>(p, stream) : nt == 2 ? launch_stream<3, 2, 2>(p, stream) : launch_stream<3, 1, 4>(p, stream);
+        else nt == 4 ? launch_stream<4, 4, 1>(p, stream) : nt == 2 ? launch_stream<4, 2, 2>(p, stream) : launch_stream<4, 1, 2>(p, stream);
+    } else {
+        const struct { int bm, bn; float us; } tile[4] = {{64, 64, 0.25f}, {128, 128, 0.70f}, {256, 128, 1.23f}, {256, 256, 2.42f}};
+        int best = 0;
+        float least = 0.f;
+        for (int i = 0; i < 4; ++i) {
+            const long long tiles = (p.M + tile[i].bm - 1LL) / tile[i].bm * ((p.N + tile[i].bn - 1LL) / tile[i].bn);
+            const float us = (float)((tiles + 255) / 256) * tile[i].us;
+            if (!i || us < least) { best = i; least = us; }
+        }
+        rc = best == 0 ? launch_tile<64, 64, 2, 2, 4>(p, stream) : best == 1 ? launch_tile<128, 128, 4, 2, 4>(p, stream) : best == 2 ? launch_tile<256, 128, 4, 2, 3>(p, stream)
+                                                                                                                         : launch_tile<256, 256, 2, 4, 2>(p, stream);
+    }
     if (rc) return rc;
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) { set_error("gemm_i8 launch: %s", hipGetErrorString(e)); return -2; }
