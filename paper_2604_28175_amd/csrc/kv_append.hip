@@ -2,10 +2,10 @@
 //
 //   dimensions (a, b) of a head at position p become (a cos - b sin, b cos + a sin), cos and sin from row p of a table; pairs (j, j + R/2) or (2j, 2j + 1)
 //
-// One launch.  Queries, and keys and values on their way into an fp16 cache, are worked on token by token: a wavefront has a token, a lane 8 numbers of a head at a
-// time, the other halves of its pairs from the cache lines that the lanes beside it read anyway.  An int8 cache has a scale for each page and head, so there a
-// wavefront has what a step brings of one page and head (of K or of V): the largest magnitude first, then the page's older codes where the scale grows,
-// then the new codes; nothing is shared between wavefronts, and no order changes a result.
+// One launch.  Queries, and keys and values on their way into an fp16 cache, are worked on token by token: a wavefront or a workgroup has a token, a thread 8 numbers of a head at a
+// time, the other halves of its pairs from the cache lines that the threads beside it read anyway.  An int8 cache has a scale for each page and head, so there a
+// wavefront (up to 128 pieces of 8 numbers: steps of single tokens) or a workgroup has what a step brings of one page and head, of K or of V: the numbers stay in registers
+// from the largest magnitude to their codes, and the page's older codes follow where the scale grows.  Nothing is shared between items, and no order changes a result.
 // Every number moves once, 2 bytes in and 1 or 2 out: the memory bounds it, and a step of single tokens is a launch's latency.
 #include "decoder.hpp"
 
@@ -83,16 +83,59 @@ __device__ __forceinline__ int sequence_of(const strait_kv_batch& b, int t) {
     return ended < b.seqs && b.q_start[ended] <= t ? ended : -1;
 }
 
-// Items: first the int8 cache's (sequence, page of the step, head, K or V), then tokens; a wavefront each.
-template <bool I8>
-__global__ void __launch_bounds__(256) kv_append_kernel(const KvAppend p, int page_items, int pages_each) {
-    if (p.hp) __builtin_amdgcn_s_setprio(3);
+// Of the pages that the step's tokens come to lie on, sequence after sequence, the index-th one: its sequence, and its place among the sequence's (false: there are fewer).
+__device__ __forceinline__ bool find_page(const strait_kv_batch& batch, int P, int index, int& b, int& c) {
     const int lane = threadIdx.x & 63;
-    const int item = __builtin_amdgcn_readfirstlane((int)blockIdx.x * 4 + (int)(threadIdx.x >> 6));
+    for (int s0 = 0; s0 < batch.seqs; s0 += 64) {
+        int n = 0;
+        if (s0 + lane < batch.seqs) {
+            const Sequence s = sequence(batch, s0 + lane);
+            const int begin = s.past < 0 ? 0 : s.past, end = s.past + s.n;
+            n = end > begin ? (end - 1) / P - begin / P + 1 : 0;
+        }
+        int upto = n;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int v = __shfl_up(upto, d);
+            upto += lane >= d ? v : 0;
+        }
+        const int all = __builtin_amdgcn_readlane(upto, 63);
+        if (index < all) {
+            const int at = __builtin_ctzll(__ballot(upto > index));
+            b = s0 + at;
+            c = index - __builtin_amdgcn_readlane(upto - n, at);
+            return true;
+        }
+        index -= all;
+    }
+    return false;
+}
+
+struct AppendGrid {
+    int blocks;              // workgroups of the int8 cache's items
+    int items;               // (page of the step, head, K or V)
+    int pages_each;          // pages that a sequence can come to lie on, each with an item; 0: the items are found by counting
+    int token_threads;       // of a token: 64 or 256
+    Divisor by_heads, by_pages_each;
+};
+
+// Workgroups: first the int8 cache's items, of TPI threads each, which hold ITER pieces of 8 numbers; then tokens.
+template <bool I8, int TPI, int ITER>
+__global__ void __launch_bounds__(256) kv_append_kernel(const KvAppend p, const AppendGrid grid) {
+    __shared__ float part[4];
+    if (p.hp) __builtin_amdgcn_s_setprio(3);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int D = p.cache.head_dim, P = p.cache.page_tokens, H = p.cache.kv_heads;
-    const int per = D / 8;                              // lanes that hold a head
-    if (I8 && item < page_items) {
-        const int v = item & 1, h = (item >> 1) % H, c = (item >> 1) / H % pages_each, b = (item >> 1) / H / pages_each;
+    const int shift = D == 128 ? 4 : 3, per = 1 << shift;               // threads that hold a head
+    if (I8 && (int)blockIdx.x < grid.blocks) {
+        const int item = TPI == 256 ? (int)blockIdx.x : (int)blockIdx.x * 4 + wave;
+        if (item >= grid.items) return;
+        const int v = item & 1, i1 = divide(item >> 1, grid.by_heads), h = (item >> 1) - i1 * H;
+        int b, c;
+        if (grid.pages_each) {
+            b = divide(i1, grid.by_pages_each);
+            c = i1 - b * grid.pages_each;
+        } else if (!find_page(p.batch, P, i1, b, c)) return;
         const Sequence s = sequence(p.batch, b);
         const int begin = s.past < 0 ? 0 : s.past, end = s.past + s.n;      // positions that are stored
         const int column = begin / P + c;
@@ -103,39 +146,61 @@ __global__ void __launch_bounds__(256) kv_append_kernel(const KvAppend p, int pa
         const long long place = (long long)page * H + h;
         int8_t* codes = (int8_t*)(v ? p.cache.v : p.cache.k) + place * P * D;
         float* scale = (v ? p.cache.v_scale : p.cache.k_scale) + place;
+        const float old_scale = *scale;
         const half_t* x = (v ? p.v : p.k) + h * D;
         const long long pitch = v ? p.pitch_v : p.pitch_k;
-        const int d = lane % per * 8, sub = lane / per, rows = 64 / per;
-        auto number = [&](int position) __attribute__((always_inline)) {
-            return rotated<true>(x + (long long)(s.first + position - s.past) * pitch, d, p.rope && !v ? p.rope + (long long)position * p.rope_dim : nullptr, p.rope_dim, p.interleaved);
-        };
+        const int t = TPI == 256 ? (int)threadIdx.x : lane, d = (t & (per - 1)) * 8, sub = t >> shift, rows = TPI >> shift;
+        Eight e[ITER];
         float top = 0.f;
-        for (int t = lo + sub; t < hi; t += rows) {
-            const Eight e = number(t);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) top = __builtin_fmaxf(top, __builtin_fabsf(e.v[i]));
+        for (int i = 0; i < ITER; ++i) {
+            const int position = lo + sub + i * rows;
+            if (position < hi)
+                e[i] = rotated<true>(x + (long long)(s.first + position - s.past) * pitch, d, p.rope && !v ? p.rope + (long long)position * p.rope_dim : nullptr, p.rope_dim, p.interleaved);
         }
 #pragma unroll
+        for (int i = 0; i < ITER; ++i)
+            if (lo + sub + i * rows < hi) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) top = __builtin_fmaxf(top, __builtin_fabsf(e[i].v[k]));
+            }
+#pragma unroll
         for (int i = 32; i; i >>= 1) top = __builtin_fmaxf(top, __shfl_xor(top, i));
+        if (TPI == 256) {
+            if (lane == 0) part[wave] = top;
+            __syncthreads();
+            top = __builtin_fmaxf(__builtin_fmaxf(part[0], part[1]), __builtin_fmaxf(part[2], part[3]));
+        }
         const bool fresh = lo == column * P;
-        const float before = fresh ? 0.f : *scale, candidate = top * (1.f / 127.f), now = candidate > before ? candidate : before;
+        const float before = fresh ? 0.f : old_scale, candidate = top * (1.f / 127.f), now = candidate > before ? candidate : before;
         if (!fresh && now > before) {
             const float by = before / now;
-            for (int t = column * P + sub; t < lo; t += rows) {
-                uintx2* at = (uintx2*)(codes + (t - column * P) * D + d);
-                const uintx2 w = *at;
-                float old[8];
+            uintx2* at = (uintx2*)(codes + d);
+            for (int r0 = sub; r0 < lo - column * P; r0 += 4 * rows) {       // (four rows under way)
+                uintx2 w[4];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) old[i] = (float)(int8_t)(w[i >> 2] >> (8 * (i & 3)));
-                *at = codes_of(old, by);
+                for (int k = 0; k < 4; ++k)
+                    if (r0 + k * rows < lo - column * P) w[k] = at[(r0 + k * rows) << shift];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if (r0 + k * rows >= lo - column * P) continue;
+                    float old[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) old[i] = (float)(int8_t)(w[k][i >> 2] >> (8 * (i & 3)));
+                    at[(r0 + k * rows) << shift] = codes_of(old, by);
+                }
             }
         }
         const float inverse = now > 0.f ? 1.f / now : 0.f;
-        for (int t = lo + sub; t < hi; t += rows) *(uintx2*)(codes + (t - column * P) * D + d) = codes_of(number(t).v, inverse);
-        if (lane == 0) *scale = now;
+#pragma unroll
+        for (int i = 0; i < ITER; ++i) {
+            const int position = lo + sub + i * rows;
+            if (position < hi) *(uintx2*)(codes + (position - column * P) * D + d) = codes_of(e[i].v, inverse);
+        }
+        if (t == 0) *scale = now;
         return;
     }
-    const int t = item - page_items;
+    const int first = (int)blockIdx.x - grid.blocks, t = grid.token_threads == 256 ? first : first * 4 + wave;
     if (t >= p.batch.tokens) return;
     const int b = sequence_of(p.batch, t);
     if (b < 0) return;
@@ -143,30 +208,51 @@ __global__ void __launch_bounds__(256) kv_append_kernel(const KvAppend p, int pa
     const int i = t - s.first, position = s.past + i;
     if (i < 0 || i >= s.n) return;
     const float* rope = p.rope && position >= 0 ? p.rope + (long long)position * p.rope_dim : nullptr;
-    for (int c = lane; c < p.heads * per; c += 64) {
-        const int h = c / per, d = c % per * 8;
-        store_half8(p.q_out + ((long long)t * p.heads + h) * D + d, rotated<false>(p.q + t * p.pitch_q + h * D, d, rope, p.rope_dim, p.interleaved));
+    // pieces of 8 numbers: the queries', then, of an fp16 cache, the keys' and the values'
+    const int nq = p.heads << shift, nkv = H << shift;
+    int column = 0, page = -1;
+    if (!I8 && position >= 0) {
+        column = position / P;
+        page = p.batch.page_table[(long long)b * p.batch.table_pitch + column];
     }
-    if (I8 || position < 0) return;
-    const int column = position / P;
-    const int page = p.batch.page_table[(long long)b * p.batch.table_pitch + column];
-    if ((unsigned)page >= (unsigned)p.cache.pages) return;
-    for (int c = lane; c < 2 * H * per; c += 64) {
-        const int v = c >= H * per, r = v ? c - H * per : c, h = r / per, d = r % per * 8;
-        half_t* at = (half_t*)(v ? p.cache.v : p.cache.k) + (((long long)page * H + h) * P + position - column * P) * D + d;
-        store_half8(at, rotated<false>((v ? p.v : p.k) + t * (v ? p.pitch_v : p.pitch_k) + h * D, d, v ? nullptr : rope, p.rope_dim, p.interleaved));
+    const int all = (unsigned)page < (unsigned)p.cache.pages ? nq + 2 * nkv : nq;
+    const long long row0 = (long long)page * H * P + position - column * P;
+    for (int c = threadIdx.x & (grid.token_threads - 1); c < all; c += grid.token_threads) {
+        const int what = c < nq ? 0 : c < nq + nkv ? 1 : 2, r = what == 0 ? c : what == 1 ? c - nq : c - nq - nkv, h = r >> shift, d = (r & (per - 1)) * 8;
+        const half_t* x = what == 0 ? p.q + t * p.pitch_q : what == 1 ? p.k + t * p.pitch_k : p.v + t * p.pitch_v;
+        half_t* at = what == 0 ? p.q_out + ((long long)t * p.heads + h) * D : (half_t*)(what == 1 ? p.cache.k : p.cache.v) + (row0 + (long long)h * P) * D;
+        store_half8(at + d, rotated<false>(x + h * D, d, what == 2 ? nullptr : rope, p.rope_dim, p.interleaved));
     }
 }
 
 int launch_kv_append(const KvAppend& p, hipStream_t stream) {
     const bool i8 = p.cache.type == STRAIT_KV_I8;
-    const int pages_each = (p.batch.max_q + p.cache.page_tokens - 2) / p.cache.page_tokens + 1;     // that a sequence's new tokens can touch
-    const long long page_items = i8 ? (long long)p.batch.seqs * pages_each * p.cache.kv_heads * 2 : 0;
-    const long long items = page_items + (i8 && !p.heads ? 0 : p.batch.tokens);
-    if (items > 0x7fffff00LL) { set_error("kv_append: grid too large"); return STRAIT_E_SHAPE; }
-    const dim3 grid((unsigned)((items + 3) / 4));
-    if (i8) hipLaunchKernelGGL((kv_append_kernel<true>), grid, dim3(256), 0, stream, p, (int)page_items, pages_each);
-    else hipLaunchKernelGGL((kv_append_kernel<false>), grid, dim3(256), 0, stream, p, 0, pages_each);
+    const int P = p.cache.page_tokens;
+    AppendGrid g{};
+    g.by_heads = divisor(p.cache.kv_heads);
+    const int most = p.batch.max_q < P ? p.batch.max_q : P, pieces = most * p.cache.head_dim / 8;     // of an item
+    const bool waves = pieces <= 128;
+    if (i8) {
+        // pages that a sequence's tokens can touch; all sequences' together touch no more than a page per P tokens and two for each
+        const long long each = (p.batch.max_q + P - 2) / P + 1, direct = each * p.batch.seqs, counted = p.batch.tokens / P + 2LL * p.batch.seqs;
+        if (direct <= counted) { g.pages_each = (int)each; g.by_pages_each = divisor(each); }
+        const long long items = (direct <= counted ? direct : counted) * p.cache.kv_heads * 2;
+        if (items > 0x3fffffffLL) { set_error("kv_append: grid too large"); return STRAIT_E_SHAPE; }
+        g.items = (int)items;
+        g.blocks = waves ? (g.items + 3) / 4 : g.items;
+    }
+    // A wavefront for each token, or four where the tokens are few or have two pieces for each of their threads (8000 tokens of 384 pieces 27.2 us and 32.5; 4000 of 512 27.8 and
+    // 25.9, 128 of 512 7.6 and 4.4)
+    g.token_threads = p.batch.tokens >= 2048 && (p.heads + (i8 ? 0 : 2 * p.cache.kv_heads)) * p.cache.head_dim / 8 < 512 ? 64 : 256;
+    const long long tokens = i8 && !p.heads ? 0 : g.token_threads == 64 ? (p.batch.tokens + 3) / 4 : p.batch.tokens;
+    const dim3 grid((unsigned)(g.blocks + tokens)), block(256);
+    if (!i8) hipLaunchKernelGGL((kv_append_kernel<false, 256, 1>), grid, block, 0, stream, p, g);
+    else if (pieces <= 64) hipLaunchKernelGGL((kv_append_kernel<true, 64, 1>), grid, block, 0, stream, p, g);
+    else if (waves) hipLaunchKernelGGL((kv_append_kernel<true, 64, 2>), grid, block, 0, stream, p, g);
+    else if (pieces <= 512) hipLaunchKernelGGL((kv_append_kernel<true, 256, 2>), grid, block, 0, stream, p, g);
+    else if (pieces <= 1024) hipLaunchKernelGGL((kv_append_kernel<true, 256, 4>), grid, block, 0, stream, p, g);
+    else if (pieces <= 2048) hipLaunchKernelGGL((kv_append_kernel<true, 256, 8>), grid, block, 0, stream, p, g);
+    else hipLaunchKernelGGL((kv_append_kernel<true, 256, 16>), grid, block, 0, stream, p, g);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) { set_error("kv_append launch: %s", hipGetErrorString(e)); return -2; }
     return 0;
