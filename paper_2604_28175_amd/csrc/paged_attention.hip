@@ -30,6 +30,11 @@ typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
 constexpr int KEYS = 32;                 // of a block
 constexpr int PAGED_WAVES = 4;
 
+// Bytes e and e + 1 of a word of codes (biased by 128) as fp16: 0x6400 + byte is 1024 + byte, from which one fused multiply-add takes 1152 and makes any power of two's multiple
+__device__ __forceinline__ half2_t scaled_codes(unsigned w, int e, half_t by) {
+    const half2_t u = __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, w, e ? 0x04030402u : 0x04010400u));
+    return __builtin_elementwise_fma(u, half2_t{by, by}, half2_t{(half_t)(-1152.f) * by, (half_t)(-1152.f) * by});
+}
 // Two of the 8-bit codes in `a` and `b` (biased by 128: codes ^ 0x80) as fp16 code 2^-9; sel: v_perm_b32's selector of the two bytes
 __device__ __forceinline__ half2_t two_codes(unsigned a, unsigned b, unsigned sel) {
     const half2_t u = __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(b, a, sel));
@@ -60,29 +65,64 @@ static int most_blocks(const PagedAttention& p, int rows) {
 
 struct PagedArgs {
     PagedAttention p;
-    int group, tiles, rows;              // query heads of a kv head; tiles of a sequence's rows and head, rows of a tile
+    int group;                           // query heads of a kv head
+    int from, to;                        // of sequences with more than `from` and at most `to` rows (new tokens times group) of a kv head
+    int tiles, rows;                     // tiles of a sequence's rows and head, rows of a tile
+    int items;                           // (sequence, tile) pairs that are found by counting; 0: each sequence has `tiles`
     int per_part, parts;                 // blocks of a part, parts at most
-    float* o; float* ml;                 // of parts: [tokens heads][parts][D] and [..][2]: the output over the sum, the maximum and the sum
-    Divisor by_group, by_heads, by_seqs, by_tiles, by_q_heads, by_max_q;
+    int join_tokens;                     // of each sequence that the join looks at; 0: it finds each token's sequence
+    int slots;                           // parts of a row that the workspace has room for
+    float* o; float* ml;                 // of parts: [tokens heads][slots][D] and [..][2]: the output over the sum, the maximum and the sum
+    Divisor by_group, by_heads, by_seqs, by_tiles, by_items, by_q_heads, by_join;
 };
 
 // A tile's rows: of sequence s, lo .. hi the positions of the first and last one.
 struct Tile { int r0, lo, hi; bool any; };
 __device__ __forceinline__ Tile tile_of(const PagedArgs& a, const Sequence& s, int tile) {
-    const int r0 = tile * a.rows, last = divide(r0 + a.rows - 1, a.by_group);
-    return {r0, s.past + divide(r0, a.by_group), s.past + (last < s.n ? last : s.n - 1), r0 < s.n * a.group};
+    const int r0 = tile * a.rows, last = divide(r0 + a.rows - 1, a.by_group), rows = s.n * a.group;
+    return {r0, s.past + divide(r0, a.by_group), s.past + (last < s.n ? last : s.n - 1), r0 < rows && rows > a.from && rows <= a.to};
 }
 
-// Workgroup ((part tiles + tile) seqs + b') heads + h: every sequence's first part comes before any second one, and a head stays on a chiplet where there are 8.  The
-// hardware deals workgroups out to the parts of a chiplet in turn and in order, one that is full holding up the others; so that no part of it gets the longest sequence
-// of every round, the sequences are moved on by one from round to round (chunks of four prompts: 0.56 -> 0.85 of the places busy).
-__device__ __forceinline__ void place_item(const PagedArgs& a, int item, int& h, int& b, int& part, int& tile) {
-    const int i1 = divide(item, a.by_heads), i2 = divide(i1, a.by_seqs);
+// Workgroup ((part tiles + tile) seqs + b') heads + h: every sequence's first part comes before any second one, a sequence's last tile, which sees the most keys, before the others,
+// and a head stays on a chiplet where there are 8.  The hardware deals workgroups out to the parts of a chiplet in turn and in order, one that is full holding up the others; so
+// that no part of it gets the longest sequence of every round, the sequences are moved on by one from round to round (chunks of four prompts: 0.56 -> 0.85 of the places busy).
+// Where sequences bring uneven numbers of tokens most of those workgroups would have none: then (part items + item) heads + h, the item-th of the tiles that there are, found by counting.
+__device__ __forceinline__ bool place_item(const PagedArgs& a, int item, int& h, int& b, int& part, int& tile) {
+    const int i1 = divide(item, a.by_heads);
     h = item - i1 * a.p.cache.kv_heads;
-    b = i1 - i2 * a.p.batch.seqs + i2 - divide(i2, a.by_seqs) * a.p.batch.seqs;
-    if (b >= a.p.batch.seqs) b -= a.p.batch.seqs;
-    part = divide(i2, a.by_tiles);
-    tile = i2 - part * a.tiles;
+    if (!a.items) {
+        const int i2 = divide(i1, a.by_seqs);
+        b = i1 - i2 * a.p.batch.seqs + i2 - divide(i2, a.by_seqs) * a.p.batch.seqs;
+        if (b >= a.p.batch.seqs) b -= a.p.batch.seqs;
+        part = divide(i2, a.by_tiles);
+        tile = a.tiles - 1 - (i2 - part * a.tiles);
+        return true;
+    }
+    part = divide(i1, a.by_items);
+    int index = i1 - part * a.items;
+    const int lane = threadIdx.x & 63;
+    for (int s0 = 0; s0 < a.p.batch.seqs; s0 += 64) {
+        int n = 0;
+        if (s0 + lane < a.p.batch.seqs) {
+            const int rows = sequence(a.p.batch, s0 + lane).n * a.group;
+            n = rows > a.from && rows <= a.to ? (rows + a.rows - 1) / a.rows : 0;
+        }
+        int upto = n;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int v = __shfl_up(upto, d);
+            upto += lane >= d ? v : 0;
+        }
+        const int all = __builtin_amdgcn_readlane(upto, 63);
+        if (index < all) {
+            const int at = __builtin_ctzll(__ballot(upto > index));
+            b = s0 + at;
+            tile = __builtin_amdgcn_readlane(upto, at) - 1 - index;
+            return true;
+        }
+        index -= all;
+    }
+    return false;
 }
 
 // A block's bytes as they come from memory: keys 16 kb + l16 at 16-byte pieces of their dimensions, and the values of 8 keys at J dimensions.
@@ -119,7 +159,7 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_stream_kernel(const
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l16 = lane & 15, g4 = lane >> 4;
     const int H = p.cache.kv_heads, P = p.cache.page_tokens;
     int h, b, part, tile;
-    place_item(a, (int)blockIdx.x, h, b, part, tile);
+    if (!place_item(a, (int)blockIdx.x, h, b, part, tile)) return;
     const Sequence s = sequence(p.batch, b);
     const Tile t = tile_of(a, s, tile);
     if (!t.any) return;
@@ -336,7 +376,7 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_stream_kernel(const
                 else *(uint2*)(out + J * (4 * g4 + v)) = *(const uint2*)y;
             }
         } else {
-            const long long slot = row * a.parts + part;
+            const long long slot = row * a.slots + part;
             float* out = a.o + slot * D;
 #pragma unroll
             for (int v = 0; v < 4; ++v)
@@ -373,8 +413,7 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, lh = lane >> 5;
     const int H = p.cache.kv_heads, P = p.cache.page_tokens;
     int h, b, part, tile;
-    place_item(a, (int)blockIdx.x, h, b, part, tile);
-    tile = a.tiles - 1 - tile;                         // the last tiles see the most keys and go first
+    if (!place_item(a, (int)blockIdx.x, h, b, part, tile)) return;
     const Sequence s = sequence(p.batch, b);
     const Tile t = tile_of(a, s, tile);
     if (!t.any) return;
@@ -399,7 +438,7 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
 #pragma unroll
         for (int v = 0; v < 16; ++v) o[db][v] = 0.f;
     float m = -INFINITY, l = 0.f;
-    const float c = p.scale * 1.44269504088896340736f * (I8 ? 512.f : 1.f);
+    const float c = p.scale * 1.44269504088896340736f;
 
     // ---- memory -> registers -> LDS.  Chunk q of 16 bytes of row r lies at q ^ (r % 16) for K (D = 64: r % 8), whose operand is 16 rows at one chunk.  V's
     // operand is 4 rows at 4 chunks at a time: the rows' bits go to the chunk's bits above those (and to the lowest, for the sake of the stores)
@@ -419,10 +458,11 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
                 places = page * H + h;
                 if (I8) {
                     kcs = fmaxf(p.cache.k_scale[places], 0x1p-100f) * c;       // (a scale of 0 belongs to codes of 0; times it, minus infinity were none)
-                    // a value is code 2^(f - 9), exact in fp16, f between -15 and 15; the rest of its scale goes into the probabilities
-                    const float vs = p.cache.v_scale[places] * 512.f;
+                    // a value is code 2^f, exact in fp16, f between -24 and 5 (1152 2^f is a number of fp16 too); the rest of its scale, between 1 and 2 for scales of 2^-24 to 64, goes into
+                    // the probabilities (fp16 numbers have scales of 516 at most: 16 times 2^8)
+                    const float vs = p.cache.v_scale[places];
                     vpow = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, vs) & 0x7f800000u);
-                    vpow = vs == 0.f ? 0.f : fminf(fmaxf(vpow, 0x1p-15f), 0x1p15f);
+                    vpow = vs == 0.f ? 0.f : fminf(fmaxf(vpow, 0x1p-24f), 0x1p5f);
                     const float ratio = vs == 0.f ? 1.f : vs / vpow;
                     vlog = __builtin_amdgcn_logf(ratio);
                     vinv = 1.f / ratio;
@@ -455,12 +495,11 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
             const int swz = v ? vswz(row) : kswz(row);
             if constexpr (I8) {
                 const uintx4 w = raw[x] ^ 0x80808080u;
-                const half_t by = (half_t)of_blockf(vpow, __builtin_amdgcn_readfirstlane(n + (row >> 5)));
+                const half_t by = v ? (half_t)of_blockf(vpow, __builtin_amdgcn_readfirstlane(n + (row >> 5))) : (half_t)1.f;
                 half8 y[2];
 #pragma unroll
                 for (int e = 0; e < 16; e += 2) {
-                    half2_t z = two_codes(w[e >> 2], 0, e & 2 ? 0x0c030c02u : 0x0c010c00u);
-                    if (v) z = z * half2_t{by, by};
+                    const half2_t z = scaled_codes(w[e >> 2], e & 2, by);
                     y[e >> 3][e & 7] = z[0];
                     y[e >> 3][(e & 7) + 1] = z[1];
                 }
@@ -611,7 +650,7 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
                 if (token >= 0) *(uintx4*)(out + db * 32 + 8 * (g + lh)) = uintx4{x[0], y[0], x[1], y[1]};
             }
     } else if (token >= 0) {
-        const long long slot = row * a.parts + part;
+        const long long slot = row * a.slots + part;
 #pragma unroll
         for (int db = 0; db < D / 32; ++db)
 #pragma unroll
@@ -622,24 +661,37 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
 
 // Joins the parts of rows that were shared out: a workgroup per (token, head), whose threads take 4 dimensions each and every few parts.
 template <int D>
-__global__ void __launch_bounds__(256) paged_join_kernel(const PagedArgs a) {
+__global__ void __launch_bounds__(256) paged_join_kernel(const PagedArgs few, const PagedArgs many) {
     constexpr int GROUP = D / 4, GROUPS = 256 / GROUP;
     __shared__ floatx4 sums[GROUPS][GROUP];
-    const PagedAttention& p = a.p;
+    const PagedAttention& p = few.p;
     if (p.hp) __builtin_amdgcn_s_setprio(3);
     const int lane = threadIdx.x & 63;
-    const int bi = divide((int)blockIdx.x, a.by_q_heads), hq = (int)blockIdx.x - bi * p.heads, b = divide(bi, a.by_max_q), i = bi - b * p.batch.max_q;
+    const int bi = divide((int)blockIdx.x, few.by_q_heads), hq = (int)blockIdx.x - bi * p.heads;
+    int b, i;
+    if (few.join_tokens) {                             // of each sequence the first few tokens
+        b = divide(bi, few.by_join);
+        i = bi - b * few.join_tokens;
+    } else {                                           // each token
+        int ended = 0;
+        for (int s0 = 0; s0 < p.batch.seqs; s0 += 64) ended += __popcll(__ballot(s0 + lane < p.batch.seqs && p.batch.q_start[s0 + lane + 1] <= bi));
+        b = ended;
+        if (b >= p.batch.seqs) return;
+        i = bi - p.batch.q_start[b];
+        if (i < 0) return;
+    }
     const Sequence s = sequence(p.batch, b);
     if (i >= s.n) return;
+    const PagedArgs& a = s.n * few.group <= few.to ? few : many;
     const int g = hq - divide(hq, a.by_group) * a.group;
     const Tile t = tile_of(a, s, (i * a.group + g) / a.rows);
     const Blocks blocks = visible_blocks(t.lo, t.hi, p.window, p.sinks);
     const int parts = (blocks.count + a.per_part - 1) / a.per_part;
     if (parts <= 1) return;
     const long long row = (long long)(s.first + i) * p.heads + hq;
-    const float2* ml = (const float2*)a.ml + row * a.parts;
+    const float2* ml = (const float2*)a.ml + row * a.slots;
     const int group = (int)threadIdx.x / GROUP, d = (int)threadIdx.x % GROUP;
-    const floatx4* o = (const floatx4*)(a.o + row * a.parts * D) + d;
+    const floatx4* o = (const floatx4*)(a.o + row * a.slots * D) + d;
     // (every wavefront finds the maximum and the sum for itself)
     float top = -INFINITY, sum = 0.f;
     for (int x = lane; x < parts; x += 64) top = fmaxf(top, ml[x].x);
@@ -675,60 +727,77 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const PagedArgs a) {
     *(uint2*)(p.out + row * D + d * 4) = *(const uint2*)h;
 }
 
-// How a call is launched.  Up to 32 rows of a sequence and kv head: the stream kernel, tiles of 16 or 32 rows.  More: the tile kernel, 128 rows, of
-// which a compute unit holds two.  (256 rows by eight wavefronts fill LDS half as often, but all of them stand at one barrier: chunks of four prompts 274 and 274 us, with a
-// window 74 and 97.)  Parts of as many blocks as give each compute unit several workgroups (tile kernel: one).
-static PagedArgs paged_plan(const PagedAttention& p) {
-    PagedArgs a{};
-    a.p = p;
-    a.group = p.heads / p.cache.kv_heads;
-    const long long rows = (long long)p.batch.max_q * a.group, pairs = (long long)p.batch.seqs * p.cache.kv_heads;
-    const bool stream = rows <= 32;
-    a.rows = rows <= 16 ? 16 : stream ? 32 : 128;
+// How a call is launched.  Sequences with up to 16 or 32 rows of a kv head: the stream kernel, tiles of 16 or 32 rows.  More: the tile kernel, 128 rows, of which a compute unit holds
+// two.  (256 rows by eight wavefronts fill LDS half as often, but all of them stand at one barrier: chunks of four prompts 274 and 274 us, with a window 74 and 97.)  A step of
+// both kinds gets both launches.  Parts of as many blocks as give each compute unit several workgroups (tile kernel: where it would not have one).
+struct PagedPlan { PagedArgs few, many; size_t workspace; long long joins; };
+
+static void plan_class(PagedArgs& a, bool stream) {
+    const PagedAttention& p = a.p;
+    const long long rows = std::min<long long>((long long)p.batch.max_q * a.group, a.to);
     a.tiles = (int)((rows + a.rows - 1) / a.rows);
+    const long long direct = (long long)p.batch.seqs * a.tiles, counted = (long long)p.batch.tokens * a.group / a.rows + p.batch.seqs;
+    a.items = direct > 2 * counted ? (int)counted : 0;
     const int most = most_blocks(p, a.rows);
-    const long long work = pairs * a.tiles * most;
-    const long long per = (work + (stream ? 2047 : 511)) / (stream ? 2048 : 512);
-    a.per_part = (int)std::min<long long>(most, std::max<long long>(stream ? 8 : 16, (per + PAGED_WAVES - 1) / PAGED_WAVES * PAGED_WAVES));
-    if (!stream && pairs * a.tiles >= 256) a.per_part = most;
+    const long long work = std::min(direct, counted) * p.cache.kv_heads * most, aim = stream ? 2048 : 512;
+    a.per_part = (int)std::min<long long>(most, std::max<long long>(stream ? 8 : 16, ((work + aim - 1) / aim + PAGED_WAVES - 1) / PAGED_WAVES * PAGED_WAVES));
+    if (!stream && std::min(direct, counted) * p.cache.kv_heads >= 256) a.per_part = most;
     a.parts = (most + a.per_part - 1) / a.per_part;
-    a.by_group = divisor(a.group); a.by_heads = divisor(p.cache.kv_heads); a.by_seqs = divisor(p.batch.seqs); a.by_tiles = divisor(a.tiles); a.by_q_heads = divisor(p.heads); a.by_max_q = divisor(p.batch.max_q);
-    a.ml = p.ws;
-    const size_t head = ((size_t)p.batch.tokens * p.heads * a.parts * 2 * sizeof(float) + 15) / 16 * 16;
-    a.o = (float*)((char*)p.ws + head);
-    return a;
+    a.by_tiles = divisor(a.tiles);
+    a.by_items = divisor(a.items);
+}
+static long long paged_grid(const PagedArgs& a) { return a.tiles ? (a.items ? a.items : (long long)a.p.batch.seqs * a.tiles) * a.p.cache.kv_heads * a.parts : 0; }
+
+static PagedPlan paged_plan(const PagedAttention& p) {
+    PagedPlan r{};
+    PagedArgs& few = r.few;
+    few.p = p;
+    few.group = p.heads / p.cache.kv_heads;
+    few.by_group = divisor(few.group); few.by_heads = divisor(p.cache.kv_heads); few.by_seqs = divisor(p.batch.seqs); few.by_q_heads = divisor(p.heads);
+    r.many = few;
+    const long long rows = (long long)p.batch.max_q * few.group;
+    // (single tokens beside prompts' chunks are worth launches of their own where their caches may be long: taken to be there if the sequences but for the longest bring few tokens)
+    const bool singles = p.batch.seqs > 1 && p.batch.tokens - p.batch.max_q <= 128LL * (p.batch.seqs - 1) && p.batch.max_kv > 512;
+    few.to = rows <= 32 ? 32 : few.group > 32 || !singles ? 0 : few.group > 16 ? 32 : 16;
+    few.rows = std::min<long long>(rows, few.to) <= 16 ? 16 : 32;
+    r.many.from = few.to; r.many.to = 0x7fffffff; r.many.rows = 128;
+    if (few.to) plan_class(few, true);
+    if (rows > few.to) plan_class(r.many, false);
+    few.slots = r.many.slots = std::max(few.parts, r.many.parts);
+    if (few.slots > 1) {
+        // the rows to be joined: the first few tokens of each sequence, or all where tiles were shared out too
+        few.join_tokens = r.many.parts > 1 ? 0 : (int)std::min<long long>(p.batch.max_q, std::max(1, few.to / few.group));
+        few.by_join = divisor(few.join_tokens);
+        r.joins = (few.join_tokens ? (long long)p.batch.seqs * few.join_tokens : p.batch.tokens) * p.heads;
+        const size_t slots = (size_t)p.batch.tokens * p.heads * few.slots, head = (slots * 2 * sizeof(float) + 15) / 16 * 16;
+        r.workspace = head + slots * p.cache.head_dim * sizeof(float);
+        few.ml = r.many.ml = p.ws;
+        few.o = r.many.o = (float*)((char*)p.ws + head);
+    }
+    return r;
 }
 
-size_t paged_attention_workspace(const PagedAttention& p) {
-    const PagedArgs a = paged_plan(p);
-    if (a.parts <= 1) return 0;
-    const size_t slots = (size_t)p.batch.tokens * p.heads * a.parts;
-    return (slots * 2 * sizeof(float) + 15) / 16 * 16 + slots * p.cache.head_dim * sizeof(float);
-}
+size_t paged_attention_workspace(const PagedAttention& p) { return paged_plan(p).workspace; }
 
 template <int D, bool I8>
-static void launch_paged(const PagedArgs& a, unsigned grid, hipStream_t stream) {
-    if (a.rows <= 32) {
-        auto kernel = a.rows == 16 ? paged_stream_kernel<D, I8, 1> : paged_stream_kernel<D, I8, 2>;
-        hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * PAGED_WAVES), 0, stream, a);
-    } else {
-        constexpr unsigned lds = 2 * 2 * TILE_KEYS * D * 2;
-        static_assert(lds <= 64 * 1024, "what a kernel may have unasked");
-        hipLaunchKernelGGL((paged_tile_kernel<D, I8>), dim3(grid), dim3(64 * PAGED_WAVES), lds, stream, a);
+static void launch_paged(const PagedPlan& r, unsigned few, unsigned many, unsigned joins, hipStream_t stream) {
+    constexpr unsigned lds = 2 * 2 * TILE_KEYS * D * 2;
+    static_assert(lds <= 64 * 1024, "what a kernel may have unasked");
+    if (many) hipLaunchKernelGGL((paged_tile_kernel<D, I8>), dim3(many), dim3(64 * PAGED_WAVES), lds, stream, r.many);
+    if (few) {
+        auto kernel = r.few.rows == 16 ? paged_stream_kernel<D, I8, 1> : paged_stream_kernel<D, I8, 2>;
+        hipLaunchKernelGGL(kernel, dim3(few), dim3(64 * PAGED_WAVES), 0, stream, r.few);
     }
+    if (joins) hipLaunchKernelGGL(paged_join_kernel<D>, dim3(joins), dim3(256), 0, stream, r.few, r.many);
 }
 
 int launch_paged_attention(const PagedAttention& p, hipStream_t stream) {
-    const PagedArgs a = paged_plan(p);
-    const long long grid = (long long)p.batch.seqs * p.cache.kv_heads * a.tiles * a.parts, joins = (long long)p.batch.seqs * p.batch.max_q * p.heads;
-    if (grid > 0x7fffffffLL || (a.parts > 1 && joins > 0x7fffffffLL)) { set_error("attention_paged: grid too large"); return STRAIT_E_SHAPE; }
+    const PagedPlan r = paged_plan(p);
+    const long long few = paged_grid(r.few), many = paged_grid(r.many), joins = r.joins;
+    if (few > 0x7fffffffLL || many > 0x7fffffffLL || joins > 0x7fffffffLL) { set_error("attention_paged: grid too large"); return STRAIT_E_SHAPE; }
     const bool i8 = p.cache.type == STRAIT_KV_I8;
-    if (p.cache.head_dim == 64) i8 ? launch_paged<64, true>(a, (unsigned)grid, stream) : launch_paged<64, false>(a, (unsigned)grid, stream);
-    else i8 ? launch_paged<128, true>(a, (unsigned)grid, stream) : launch_paged<128, false>(a, (unsigned)grid, stream);
-    if (a.parts > 1) {
-        auto join = p.cache.head_dim == 64 ? paged_join_kernel<64> : paged_join_kernel<128>;
-        hipLaunchKernelGGL(join, dim3((unsigned)joins), dim3(256), 0, stream, a);
-    }
+    if (p.cache.head_dim == 64) i8 ? launch_paged<64, true>(r, (unsigned)few, (unsigned)many, (unsigned)joins, stream) : launch_paged<64, false>(r, (unsigned)few, (unsigned)many, (unsigned)joins, stream);
+    else i8 ? launch_paged<128, true>(r, (unsigned)few, (unsigned)many, (unsigned)joins, stream) : launch_paged<128, false>(r, (unsigned)few, (unsigned)many, (unsigned)joins, stream);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) { set_error("attention_paged launch: %s", hipGetErrorString(e)); return -2; }
     return 0;
