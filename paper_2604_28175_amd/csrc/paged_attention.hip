@@ -445,22 +445,28 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
     auto kswz = [](int row) { return D == 128 ? row & 15 : row & 7; };
     auto vswz = [](int row) { return D == 128 ? (row & 3) << 2 | (row & 1) : (row & 2) << 1; };
     uintx4 raw[NI];
-    // a lane of each wavefront holds what is to be known of a block: where it begins, its place (-1: not seen), and its scales
-    int k0s = 0, places = -1;
+    // A lane of each wavefront holds what is to be known of a block: where it begins (behind all rows: not seen) and lies in the cache, and its scales; two masks say
+    // which of the 64 blocks all of the wavefront's rows see whole, and which none of them sees.
+    int k0s = 0;
+    unsigned from_lo = 0, from_hi = 0;
     float kcs = c, vpow = 1.f, vlog = 0.f, vinv = 1.f;
+    unsigned long long full = 0, none = 0;
     auto look_up = [&](int first) __attribute__((always_inline)) {
         k0s = 0x7fffff00;
-        places = -1;
+        from_lo = from_hi = 0;
         if (first + lane < end) {
             const int k0 = blocks.at(first + lane) * KEYS, page = p.batch.page_table[(long long)b * p.batch.table_pitch + k0 / P];
             if ((unsigned)page < (unsigned)p.cache.pages) {
+                const int place = page * H + h;
+                const unsigned long long from = ((unsigned long long)place * P + (k0 & (P - 1))) * (D * ES);
                 k0s = k0;
-                places = page * H + h;
+                from_lo = (unsigned)from;
+                from_hi = (unsigned)(from >> 32);
                 if (I8) {
-                    kcs = fmaxf(p.cache.k_scale[places], 0x1p-100f) * c;       // (a scale of 0 belongs to codes of 0; times it, minus infinity were none)
+                    kcs = fmaxf(p.cache.k_scale[place], 0x1p-100f) * c;       // (a scale of 0 belongs to codes of 0; times it, minus infinity were none)
                     // a value is code 2^f, exact in fp16, f between -24 and 5 (1152 2^f is a number of fp16 too); the rest of its scale, between 1 and 2 for scales of 2^-24 to 64, goes into
                     // the probabilities (fp16 numbers have scales of 516 at most: 16 times 2^8)
-                    const float vs = p.cache.v_scale[places];
+                    const float vs = p.cache.v_scale[place];
                     vpow = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, vs) & 0x7f800000u);
                     vpow = vs == 0.f ? 0.f : fminf(fmaxf(vpow, 0x1p-24f), 0x1p5f);
                     const float ratio = vs == 0.f ? 1.f : vs / vpow;
@@ -469,6 +475,8 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
                 }
             }
         }
+        none = __ballot(!any || k0s > hi || (p.window && lo - (k0s + KEYS - 1) >= p.window && k0s >= p.sinks));
+        full = __ballot(k0s + KEYS - 1 <= lo && (!p.window || hi - k0s < p.window || k0s + KEYS - 1 < p.sinks));
     };
     auto of_block = [](int v, int n) __attribute__((always_inline)) { return __builtin_amdgcn_readlane(v, n); };
     auto of_blockf = [](float v, int n) __attribute__((always_inline)) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), n)); };
@@ -477,14 +485,12 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
         for (int x = 0; x < NI; ++x) {
             const int v = x * NT >= HALF, rem = x * NT + tid - v * HALF, row = rem / PER_ROW;
             const int blk = n + (PER_ROW * KEYS >= NT ? x * NT % HALF / (PER_ROW * KEYS) : __builtin_amdgcn_readfirstlane(row >> 5));
-            const int place = of_block(places, blk), k0 = of_block(k0s, blk);
-            raw[x] = uintx4{0, 0, 0, 0};
-            if (place < 0) continue;
-            const char* from = (const char*)(v ? p.cache.v : p.cache.k) + ((long long)place * P + (k0 & (P - 1))) * (D * ES);
-            const uintx4 got = *(const uintx4*)(from + (unsigned)(rem & (KEYS * PER_ROW - 1)) * 16u);
-            // (what no row of the tile sees may be anything: of fp16 it becomes zeros)
-            const int key = k0 + (row & 31);
-            raw[x] = I8 || (key <= t.hi && (!p.window || t.lo - key < p.window || key < p.sinks)) ? got : uintx4{0, 0, 0, 0};
+            const unsigned long long from = (unsigned long long)(unsigned)of_block((int)from_hi, blk) << 32 | (unsigned)of_block((int)from_lo, blk);
+            raw[x] = *(const uintx4*)((const char*)(v ? p.cache.v : p.cache.k) + from + (unsigned)(rem & (KEYS * PER_ROW - 1)) * 16u);
+            if constexpr (!I8) {                       // what no row of the tile sees may be anything: it becomes zeros (of int8 it is finite, and its probability 0)
+                const int key = of_block(k0s, blk) + (row & 31);
+                if (!(key <= t.hi && (!p.window || t.lo - key < p.window || key < p.sinks))) raw[x] = uintx4{0, 0, 0, 0};
+            }
         }
     };
     auto stage = [&](int n, int st) __attribute__((always_inline)) {
@@ -602,12 +608,7 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
         __syncthreads();
         int st = 0, n = 0;                             // tile of blocks n, n + 1 of those that were looked up
         for (int first = begin; first < end;) {
-            const int k0 = of_block(k0s, n), k1 = of_block(k0s, n + 1);
-            const bool dead = of_block(places, n) < 0 && of_block(places, n + 1) < 0;
-            // what the wavefront's rows see of the two blocks
-            auto none = [&](int k) { return k > hi || (p.window && lo - (k + KEYS - 1) >= p.window && k >= p.sinks); };
-            auto full = [&](int k) { return k + KEYS - 1 <= lo && (!p.window || hi - k < p.window || k + KEYS - 1 < p.sinks); };
-            const bool skip = !any || dead || (none(k0) && none(k1)), whole = full(k0) && full(k1);
+            const bool skip = (none >> n & 3) == 3, whole = (full >> n & 3) == 3;
             const int nn = n + 2;
             const bool more = first + 2 < end;
             // (a look-up replaces what the current tile still needs: it waits for the tile's end)
