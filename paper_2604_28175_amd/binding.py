@@ -6,7 +6,6 @@ library is missing, importing this module raises.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes as C
 import os
 from typing import Optional, Sequence
@@ -595,81 +594,96 @@ def _refuse(why: str):
     raise StraitError(E_INVALID, why)
 
 
-# (A step of single tokens is a few launches of a few microseconds each: what a call checks is checked in the cheapest order, and what is wrong is looked for only
-# where something is.)
+# A step of single tokens is a few launches of a few microseconds each, which these calls must not hold up: they check in the cheapest order and look for what is wrong only
+# where something is.
+_INT8, _FP16, _FP32, _INT32 = torch.int8, torch.float16, torch.float32, torch.int32
+
+
+def _what(t) -> str:
+    return f"{t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}" if isinstance(t, torch.Tensor) else repr(type(t))
+
+
 def _dense(t, dtype, shape, device: int, what: str):
-    """Refuses what is not a dense tensor of this type and shape (None: any size) on this GPU (-1: on any)."""
-    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and (t.shape == shape or len(shape) == t.dim() and all(a is None or a == b for a, b in zip(shape, t.shape)))
-            and t.is_contiguous() and t.is_cuda and (device < 0 or t.get_device() == device)):
-        _refuse(f"{what} must be a contiguous {dtype} tensor of shape {shape} on the GPU of the other tensors, is " +
-                (f"{t.dtype} {tuple(t.shape)} on {t.device}" if isinstance(t, torch.Tensor) else repr(type(t))))
+    """Refuses what is not a dense tensor of this type and shape on this GPU."""
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.get_device() == device and t.is_contiguous()):
+        _refuse(f"{what} must be a contiguous {dtype} tensor of shape {shape} on the GPU of the other tensors, is {_what(t)}")
 
 
-def _rows(t, width, device: int, what: str) -> int:
-    """fp16 rows [T][width] (None: any width), which may be columns of a wider tensor; the elements from one to the next."""
-    if not (isinstance(t, torch.Tensor) and t.dtype is torch.float16 and t.dim() == 2 and (width is None or t.size(1) == width) and t.is_cuda and
-            (device < 0 or t.get_device() == device) and (t.stride(1) == 1 or t.size(1) <= 1)):
-        _refuse(f"{what} must be float16 rows [tokens][{'width' if width is None else width}] of adjacent elements on the GPU of the other tensors, is " +
-                (f"{t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}" if isinstance(t, torch.Tensor) else repr(type(t))))
-    return t.stride(0) if t.size(0) > 1 else (t.size(1) + 7) // 8 * 8
+def _any_dense(t, dtype, dims: int, device: int, what: str):
+    """Likewise, of any shape of so many dimensions; device -1: on any GPU."""
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.dim() == dims and t.is_cuda and t.is_contiguous() and (device < 0 or t.get_device() == device)):
+        _refuse(f"{what} must be a contiguous {dtype} tensor of {dims} dimensions on the GPU of the other tensors, is {_what(t)}")
 
 
-_HERE = contextlib.nullcontext()
+def _rows(t, device: int, what: str) -> int:
+    """fp16 rows, which may be columns of a wider tensor; the elements from one to the next.  device -1: on any GPU."""
+    if not (isinstance(t, torch.Tensor) and t.dtype is _FP16 and t.dim() == 2 and t.is_cuda and (device < 0 or t.get_device() == device)):
+        _refuse(f"{what} must be float16 rows on the GPU of the other tensors, is {_what(t)}")
+    pitch, step = t.stride()
+    if step != 1 and t.size(1) > 1:
+        _refuse(f"the elements of a row of {what} must be adjacent, it is {_what(t)}")
+    return pitch if t.size(0) > 1 else (t.size(1) + 7) // 8 * 8
 
 
-def _on(device: int):
-    """Makes a tensor's device the current one for a call."""
-    return _HERE if torch.cuda.current_device() == device else torch.cuda.device(device)
-
-
+_device_now = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 # (the handle of a device's current stream, without a Stream object around it where torch offers that: 0.1 us instead of 1.1)
-_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+_stream_now = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
-def _stream_on(device: int, stream) -> int:
+def _elsewhere(device: int, call, *args):
+    """A call whose tensors are not on the current device, with that made the current one."""
+    with torch.cuda.device(device):
+        return call(*args)
+
+
+def _handle(device: int, stream) -> int:
     if stream is None:
-        return _current_stream(device)
+        return _stream_now(device)
     if stream.device.index != device:
         _refuse("the stream must be on the device of the tensors")
     return stream.cuda_stream
 
 
-def _made(stream, *tensors):
-    """Tells tensors that were made for a call of a stream that is not the current one."""
+def _made(stream, t):
+    """A tensor that was made for a call, told of a stream that is not the current one."""
     if stream is not None:
-        for t in tensors:
-            t.record_stream(stream)
+        t.record_stream(stream)
+    return t
 
 
 def k_quantize_rows(x, hp=0, stream=None):
     """strait_k_quantize_rows of x fp16 [M][K] (rows may lie further apart); returns (codes int8 [M][K], scale fp32 [M])."""
-    pitch = _rows(x, None, -1, "x")
-    (m, k), device = x.shape, x.get_device()
-    with _on(device):
-        handle = _stream_on(device, stream)
-        q, scale = torch.empty((m, k), dtype=torch.int8, device=x.device), torch.empty((m,), dtype=torch.float32, device=x.device)
-        _made(stream, q, scale)
-        _check(lib.strait_k_quantize_rows(handle, x.data_ptr(), m, k, pitch, q.data_ptr(), scale.data_ptr(), hp))
+    pitch = _rows(x, -1, "x")
+    device = x.get_device()
+    if _device_now() != device:
+        return _elsewhere(device, k_quantize_rows, x, hp, stream)
+    m, k = x.shape
+    handle = _handle(device, stream)
+    q, scale = _made(stream, x.new_empty((m, k), dtype=_INT8)), _made(stream, x.new_empty((m,), dtype=_FP32))
+    _check(lib.strait_k_quantize_rows(handle, x.data_ptr(), m, k, pitch, q.data_ptr(), scale.data_ptr(), hp))
     return q, scale
 
 
 def k_gemm_i8(x, x_scale, w, w_scale, bias=None, act=ACT_NONE, res=None, out_f32=False, hp=0, stream=None):
     """strait_k_gemm_i8: x int8 [M][K] and its rows' scales, w int8 [N][K] and its rows' scales; returns y [M][N]."""
-    _dense(x, torch.int8, (None, None), -1, "x")
-    (m, k), device = x.shape, x.get_device()
-    _dense(w, torch.int8, (None, k), device, "w")
-    n = w.size(0)
-    _dense(x_scale, torch.float32, (m,), device, "x_scale")
-    _dense(w_scale, torch.float32, (n,), device, "w_scale")
+    _any_dense(x, _INT8, 2, -1, "x")
+    device = x.get_device()
+    _any_dense(w, _INT8, 2, device, "w")
+    m, k = x.shape
+    n, wk = w.shape
+    if wk != k:
+        _refuse(f"x and w must have rows of one length, have {k} and {wk}")
+    _dense(x_scale, _FP32, (m,), device, "x_scale")
+    _dense(w_scale, _FP32, (n,), device, "w_scale")
     if bias is not None:
-        _dense(bias, torch.float32, (n,), device, "bias")
+        _dense(bias, _FP32, (n,), device, "bias")
     if res is not None:
-        _dense(res, torch.float16, (m, n), device, "res")
-    with _on(device):
-        handle = _stream_on(device, stream)
-        y = torch.empty((m, n), dtype=torch.float32 if out_f32 else torch.float16, device=x.device)
-        _made(stream, y)
-        _check(lib.strait_k_gemm_i8(handle, x.data_ptr(), x_scale.data_ptr(), w.data_ptr(), w_scale.data_ptr(), _dev(bias), m, n, k, act, _dev(res), y.data_ptr(), out_f32, hp))
+        _dense(res, _FP16, (m, n), device, "res")
+    if _device_now() != device:
+        return _elsewhere(device, k_gemm_i8, x, x_scale, w, w_scale, bias, act, res, out_f32, hp, stream)
+    handle = _handle(device, stream)
+    y = _made(stream, x.new_empty((m, n), dtype=_FP32 if out_f32 else _FP16))
+    _check(lib.strait_k_gemm_i8(handle, x.data_ptr(), x_scale.data_ptr(), w.data_ptr(), w_scale.data_ptr(), _dev(bias), m, n, k, act, _dev(res), y.data_ptr(), out_f32, hp))
     return y
 
 
@@ -685,17 +699,18 @@ class KvCache:
     [pages][kv_heads]."""
 
     def __init__(self, k, v, k_scale=None, v_scale=None):
-        i8 = isinstance(k, torch.Tensor) and k.dtype is torch.int8
-        _dense(k, torch.int8 if i8 else torch.float16, (None,) * 4, -1, "k")
+        i8 = isinstance(k, torch.Tensor) and k.dtype is _INT8
+        _any_dense(k, _INT8 if i8 else _FP16, 4, -1, "k")
         self.device = k.get_device()
         _dense(v, k.dtype, tuple(k.shape), self.device, "v")
         if i8 != (k_scale is not None) or i8 != (v_scale is not None):
             _refuse("an int8 cache has k_scale and v_scale, an fp16 cache none")
         if i8:
-            _dense(k_scale, torch.float32, tuple(k.shape[:2]), self.device, "k_scale")
-            _dense(v_scale, torch.float32, tuple(k.shape[:2]), self.device, "v_scale")
+            _dense(k_scale, _FP32, tuple(k.shape[:2]), self.device, "k_scale")
+            _dense(v_scale, _FP32, tuple(k.shape[:2]), self.device, "v_scale")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.pages, self.kv_heads, self.page_tokens, self.head_dim = k.shape
+        self.width = self.kv_heads * self.head_dim
         self.desc = KvCacheDesc(_dev(k), _dev(v), _dev(k_scale), _dev(v_scale), KV_I8 if i8 else KV_F16, self.pages, self.page_tokens, self.kv_heads, self.head_dim)
         self.ref = C.byref(self.desc)
 
@@ -705,10 +720,12 @@ class KvBatch:
     [seqs][columns].  How many tokens a step has is the rows of the tensors that it is called with."""
 
     def __init__(self, q_start, kv_len, page_table, max_q: int, max_kv: int):
-        _dense(kv_len, torch.int32, (None,), -1, "kv_len")
+        _any_dense(kv_len, _INT32, 1, -1, "kv_len")
         self.device = kv_len.get_device()
-        _dense(q_start, torch.int32, (kv_len.shape[0] + 1,), self.device, "q_start")
-        _dense(page_table, torch.int32, (kv_len.shape[0], None), self.device, "page_table")
+        _dense(q_start, _INT32, (kv_len.shape[0] + 1,), self.device, "q_start")
+        _any_dense(page_table, _INT32, 2, self.device, "page_table")
+        if page_table.shape[0] != kv_len.shape[0]:
+            _refuse(f"page_table has {page_table.shape[0]} rows for {kv_len.shape[0]} sequences")
         self.q_start, self.kv_len, self.page_table = q_start, kv_len, page_table
         self.desc = KvBatchDesc(_dev(q_start), _dev(kv_len), _dev(page_table), kv_len.shape[0], 0, max_q, max_kv, page_table.shape[1])
         self._of = {}
@@ -731,29 +748,29 @@ def k_kv_append(cache: KvCache, batch: KvBatch, k, v, q=None, rope=None, interle
     device, dim = cache.device, cache.head_dim
     if batch.device != device:
         _refuse("cache and batch must be on one device")
-    width = cache.kv_heads * dim
-    pk, pv = _rows(k, width, device, "k"), _rows(v, width, device, "v")
-    tokens, pq, heads, rope_rows, rope_dim = k.size(0), 0, 0, 0, 0
-    if v.size(0) != tokens:
-        _refuse("k and v have different numbers of tokens")
+    pk, pv = _rows(k, device, "k"), _rows(v, device, "v")
+    tokens, width = k.shape
+    pq = heads = rope_rows = rope_dim = 0
+    if width != cache.width or v.shape != (tokens, width):
+        _refuse(f"k and v must be [tokens][{cache.width}], are {tuple(k.shape)} and {tuple(v.shape)}")
     if rope is not None:
-        _dense(rope, torch.float32, (None, None), device, "rope")
+        _any_dense(rope, _FP32, 2, device, "rope")
         rope_rows, rope_dim = rope.shape
     if q is not None:
-        pq, heads = _rows(q, None, device, "q"), q.size(1) // dim
-        if q.size(0) != tokens or q.size(1) != heads * dim:
+        pq, heads = _rows(q, device, "q"), q.size(1) // dim
+        if q.shape != (tokens, heads * dim):
             _refuse(f"q must be [{tokens}][heads * {dim}], is {tuple(q.shape)}")
     elif q_out is not None:
         _refuse("q_out without q")
-    with _on(device):
-        handle = _stream_on(device, stream)
-        if q_out is not None:
-            _dense(q_out, torch.float16, (tokens, heads * dim), device, "q_out")
-        elif q is not None:
-            q_out = torch.empty((tokens, heads * dim), dtype=torch.float16, device=q.device)
-            _made(stream, q_out)
-        _check(lib.strait_k_kv_append(handle, cache.ref, batch.ref(tokens), _dev(q), k.data_ptr(), v.data_ptr(), pq, pk, pv, heads, _dev(rope), rope_rows, rope_dim,
-                                      interleaved, _dev(q_out), hp))
+    if _device_now() != device:
+        return _elsewhere(device, k_kv_append, cache, batch, k, v, q, rope, interleaved, q_out, hp, stream)
+    handle = _handle(device, stream)
+    if q_out is not None:
+        _dense(q_out, _FP16, (tokens, heads * dim), device, "q_out")
+    elif q is not None:
+        q_out = _made(stream, q.new_empty((tokens, heads * dim)))
+    _check(lib.strait_k_kv_append(handle, cache.ref, batch.ref(tokens), _dev(q), k.data_ptr(), v.data_ptr(), pq, pk, pv, heads, _dev(rope), rope_rows, rope_dim,
+                                  interleaved, _dev(q_out), hp))
     return q_out
 
 
@@ -763,24 +780,23 @@ def k_attention_paged(q, cache: KvCache, batch: KvBatch, scale: float, window: i
     device, dim = cache.device, cache.head_dim
     if batch.device != device:
         _refuse("cache and batch must be on one device")
-    pitch = _rows(q, None, device, "q")
+    pitch = _rows(q, device, "q")
     tokens, width = q.shape
     heads = width // dim
     if heads * dim != width:
         _refuse(f"q must be [tokens][heads * {dim}], is {tuple(q.shape)}")
-    with _on(device):
-        handle = _stream_on(device, stream)
-        if out is None:
-            out = torch.empty((tokens, width), dtype=torch.float16, device=q.device)
-            _made(stream, out)
-        else:
-            _dense(out, torch.float16, (tokens, width), device, "out")
-        need, ref, ws = _sz(), batch.ref(tokens), None
-        _check(lib.strait_k_attention_paged_workspace(cache.ref, ref, heads, window, sinks, C.byref(need)))
-        if need.value:
-            ws = torch.empty((need.value,), dtype=torch.uint8, device=q.device)
-            _made(stream, ws)
-        _check(lib.strait_k_attention_paged(handle, cache.ref, ref, q.data_ptr(), pitch, heads, scale, window, sinks, out.data_ptr(), _dev(ws), need.value, hp))
+    if _device_now() != device:
+        return _elsewhere(device, k_attention_paged, q, cache, batch, scale, window, sinks, out, hp, stream)
+    handle = _handle(device, stream)
+    if out is None:
+        out = _made(stream, q.new_empty((tokens, width)))
+    else:
+        _dense(out, _FP16, (tokens, width), device, "out")
+    need, ref, ws = _sz(), batch.ref(tokens), None
+    _check(lib.strait_k_attention_paged_workspace(cache.ref, ref, heads, window, sinks, C.byref(need)))
+    if need.value:
+        ws = _made(stream, q.new_empty((need.value // 2,)))            # (of halfs; a multiple of 16 bytes)
+    _check(lib.strait_k_attention_paged(handle, cache.ref, ref, q.data_ptr(), pitch, heads, scale, window, sinks, out.data_ptr(), _dev(ws), need.value, hp))
     return out
 
 
