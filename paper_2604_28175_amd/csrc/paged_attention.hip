@@ -740,8 +740,13 @@ static void plan_class(PagedArgs& a, bool stream) {
     const long long direct = (long long)p.batch.seqs * a.tiles, counted = (long long)p.batch.tokens * a.group / a.rows + p.batch.seqs;
     a.items = direct > 2 * counted ? (int)counted : 0;
     const int most = most_blocks(p, a.rows);
-    const long long work = std::min(direct, counted) * p.cache.kv_heads * most, aim = stream ? 2048 : 512;
-    a.per_part = (int)std::min<long long>(most, std::max<long long>(stream ? 8 : 16, ((work + aim - 1) / aim + PAGED_WAVES - 1) / PAGED_WAVES * PAGED_WAVES));
+    // Stream kernel: about 1024 parts (512 of 32 rows, whose results are more to join), but no more than 32 blocks each while there are 4096 or fewer of those: lengths differ, and
+    // what is left to the longest parts at the end is read by few compute units (24 streams of 129 blocks and 4 heads, parts of 8, 16 and 28 blocks: 53.7, 47.5 and 47.0 us; 32 sequences of
+    // 32 to 512 and 8 heads, parts of 16, 32, 64 and 128: 128, 122, 127 and 129; all of 256: 133, 115, 108 and 109).  Tile kernel: one part, or 512 where there are few tiles.
+    const long long work = std::min(direct, counted) * p.cache.kv_heads * most;
+    auto share = [&](long long n) { return ((work + n - 1) / n + PAGED_WAVES - 1) / PAGED_WAVES * PAGED_WAVES; };
+    const long long per = stream ? std::max<long long>(8, std::min(share(a.rows == 16 ? 1024 : 512), std::max<long long>(32, share(4096)))) : std::max<long long>(16, share(512));
+    a.per_part = (int)std::min<long long>(most, per);
     if (!stream && std::min(direct, counted) * p.cache.kv_heads >= 256) a.per_part = most;
     a.parts = (most + a.per_part - 1) / a.per_part;
     a.by_tiles = divisor(a.tiles);
