@@ -138,6 +138,30 @@ __global__ void __launch_bounds__(64 * WGM * WGN, (tile_waves_per_simd<BM, BN, W
     place_tile(a.order, xcd_range(a.order.tiles, blockIdx.x), tm, tn);
     const int m0 = tm * BM, n0 = tn * BN;
 
+    // a residual's part of the epilogue: LANES lanes lie along a row, 8 outputs each; on tiles of 32 rows to a wavefront all of it is requested ahead of the first slice
+    constexpr int LANES = BN / 8, ROWS = WGM * 32 / (NT / LANES);      // rows of a lane among 32 of each wavefront
+    const int c0 = tid % LANES * 8, n = n0 + c0, many = p.N - n < 8 ? p.N - n : 8;
+    half8 res[ROWS];
+    auto row_of = [&](int b, int i) __attribute__((always_inline)) {
+        const int r = i * (NT / LANES) + tid / LANES;
+        return m0 + r / 32 * TM + b * 32 + r % 32;
+    };
+    auto load_res = [&](int b) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+            const int m = row_of(b, i);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) res[i][j] = (half_t)0.f;
+            if (!p.res || m >= p.M) continue;
+            const half_t* at = p.res + (long long)m * p.N + n;
+            if (many == 8) res[i] = ((const AnyHalf8*)at)->h;
+            else
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (j < many) res[i][j] = at[j];
+        }
+    };
+    if (TMB == 1) load_res(0);
     // the tile's rows as buffers of their own: offsets stay below 256 * 131056 whatever the operands' size; rows and numbers past the end arrive as zeros
     const intx4 xrsrc = make_rsrc(p.x + (long long)m0 * p.K, (unsigned)(p.M - m0 < BM ? p.M - m0 : BM) * (unsigned)p.K);
     const intx4 wrsrc = make_rsrc(p.w + (long long)n0 * p.K, (unsigned)(p.N - n0 < BN ? p.N - n0 : BN) * (unsigned)p.K);
@@ -237,9 +261,8 @@ __global__ void __launch_bounds__(64 * WGM * WGN, (tile_waves_per_simd<BM, BN, W
     }
     // with a residual, or in fp32: the sums go through LDS, 32 rows of each wavefront at a time, and are finished by lanes that lie along a row, 8 outputs each
     int* const sums = (int*)tile_smem;
-    constexpr int LDS_N = BN + 4, LANES = BN / 8, ROWS = WGM * 32 / (NT / LANES);     // lanes along a row, rows of a lane
+    constexpr int LDS_N = BN + 4;
     static_assert(WGM * 32 * LDS_N * 4 <= (int)tile_lds<BM, BN, WGM, WGN, STAGES>() && WGM * 32 % (NT / LANES) == 0, "staging");
-    const int c0 = tid % LANES * 8, n = n0 + c0, many = p.N - n < 8 ? p.N - n : 8;
     float ws[8], bias[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -249,26 +272,10 @@ __global__ void __launch_bounds__(64 * WGM * WGN, (tile_waves_per_simd<BM, BN, W
     }
 #pragma unroll
     for (int b = 0; b < TMB; ++b) {
-        // (the residual is on its way while the sums are)
-        half8 res[ROWS];
         float xs[ROWS];
-        int ms[ROWS];
 #pragma unroll
-        for (int i = 0; i < ROWS; ++i) {
-            const int r = i * (NT / LANES) + tid / LANES;
-            const int m = ms[i] = m0 + r / 32 * TM + b * 32 + r % 32;
-            xs[i] = m < p.M ? p.xs[m] : 0.f;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) res[i][j] = (half_t)0.f;
-            if (p.res && m < p.M) {
-                const half_t* at = p.res + (long long)m * p.N + n;
-                if (many == 8) res[i] = ((const AnyHalf8*)at)->h;
-                else
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (j < many) res[i][j] = at[j];
-            }
-        }
+        for (int i = 0; i < ROWS; ++i) xs[i] = row_of(b, i) < p.M ? p.xs[row_of(b, i)] : 0.f;
+        if (TMB > 1) load_res(b);                      // (on its way while the sums are)
         if (b) __syncthreads();
 #pragma unroll
         for (int t = 0; t < TNB; ++t)
@@ -283,8 +290,9 @@ __global__ void __launch_bounds__(64 * WGM * WGN, (tile_waves_per_simd<BM, BN, W
             float y[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) y[j] = finish(j < 4 ? lo[j] : hi[j - 4], xs[i], ws[j], bias[j], (float)res[i][j], p.act);
-            if (ms[i] >= p.M || many <= 0) continue;
-            const long long at = (long long)ms[i] * p.N + n;
+            const int m = row_of(b, i);
+            if (m >= p.M || many <= 0) continue;
+            const long long at = (long long)m * p.N + n;
             if (p.out_f32) {
                 if (many == 8) {
                     *(AnyFloat4*)((float*)p.y + at) = AnyFloat4{floatx4{y[0], y[1], y[2], y[3]}};
