@@ -397,6 +397,44 @@ def test_attention_paged(S, case, window, sinks, i8):
     check_attention(S, World(S, 21, new, past, H, G, dim, page, i8), window, sinks)
 
 
+UNEVEN = [  # steps of sequences that bring very different numbers of tokens; sequences beyond the 64 that are looked at in one go
+    ([300] + [1] * 30, [0] + [i * 17 % 200 for i in range(30)], 2, 1, 64, 32),
+    ([1] * 40 + [150] + [2] * 40, [700 + i * 7 % 90 for i in range(40)] + [100] + [i for i in range(40)], 1, 3, 128, 64),
+    ([5] * 70 + [0] * 5 + [200, 1], [i * 3 for i in range(75)] + [600, 0], 1, 2, 64, 64),
+]
+
+
+@pytest.mark.parametrize("i8", [False, True], ids=["fp16", "int8"])
+@pytest.mark.parametrize("case", UNEVEN, ids=lambda c: f"{len(c[0])}seqs-{max(c[0])}new")
+def test_uneven_steps(S, case, i8):
+    new, past, H, G, dim, page = case
+    check_attention(S, World(S, 28, new, past, H, G, dim, page, i8))
+    check_attention(S, World(S, 29, new, past, H, G, dim, page, i8), 90, 5)
+    w = World(S, 30, new, past, H, G, dim, page, i8).on_gpu()
+    qkv, q, k, v, rope = append_inputs(w, 32)
+    got = S.k_kv_append(w.cache, w.batch, dev(S, k), dev(S, v), q=dev(S, q), rope=dev(S, rope), interleaved=True)
+    check_append(w, q, k, v, rope, True, host(got), w.taken_back())
+
+
+@pytest.mark.parametrize("i8", [False, True], ids=["fp16", "int8"])
+def test_attention_paged_over_long_caches(S, i8):
+    """More parts of a row than lanes, and workgroups and wavefronts with more blocks than they look up at a time."""
+    check_attention(S, World(S, 37, [1], [20000], 1, 2, 64, 64, i8))
+    check_attention(S, World(S, 38, [256], [2100], 32, 4, 64, 128, i8))
+
+
+def test_attention_paged_many_sequences_of_one_long_prompt(S):
+    w = World(S, 39, [1] * 512, [0] * 512, 8, 1, 64, 256, True)
+    pages, keys = 33, 33 * 256 - 7
+    r = w.r
+    w.k, w.v = (np.clip(np.rint(r.standard_normal((pages, 8, 256, 64)) * 36), -127, 127).astype(np.int8) for _ in range(2))
+    w.ks, w.vs = (np.exp(r.standard_normal((pages, 8)) * 0.3).astype(np.float32) * np.float32(0.03) for _ in range(2))
+    w.table = np.repeat(r.permutation(pages).astype(np.int32)[None], 512, 0)
+    w.kv_len = np.array([keys - i % 3 for i in range(512)], np.int32)
+    w.pages, w.max_kv = pages, keys
+    check_attention(S, w)
+
+
 @pytest.mark.parametrize("i8", [False, True], ids=["fp16", "int8"])
 @pytest.mark.parametrize("new,max_q", [([3, 4, 2, 6], 5), ([3, 140, 2, 6], 120)], ids=["few", "many"])
 def test_attention_paged_where_nothing_is_to_be_seen(S, i8, new, max_q):
