@@ -114,8 +114,10 @@ constexpr unsigned tile_lds() {
     return ring > out ? ring : out;
 }
 template <int BM, int BN, int WGM, int WGN, int STAGES>
+constexpr unsigned tile_lds_all() { return tile_lds<BM, BN, WGM, WGN, STAGES>() + BN * 8; }      // + the channels' scales and biases
+template <int BM, int BN, int WGM, int WGN, int STAGES>
 constexpr int tile_waves_per_simd() {
-    const int w = 160 * 1024 / (int)tile_lds<BM, BN, WGM, WGN, STAGES>() * WGM * WGN / 4;
+    const int w = 160 * 1024 / (int)tile_lds_all<BM, BN, WGM, WGN, STAGES>() * WGM * WGN / 4;
     return w < 1 ? 1 : w > 4 ? 4 : w;
 }
 
@@ -127,7 +129,7 @@ __global__ void __launch_bounds__(64 * WGM * WGN, (tile_waves_per_simd<BM, BN, W
     constexpr int XI = BM / (8 * NW), WI = BN / (8 * NW), NX = XI + WI, NM = TMB * TNB;      // transfers of 8 rows per wavefront and slice; MFMAs per step
     constexpr unsigned STAGE = (BM + BN) * SLICE;
     constexpr int LDC = BN + 8;
-    static_assert(TM % 32 == 0 && TN % 32 == 0 && BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && NW % 2 == 0 && STAGES >= 2 && tile_lds<BM, BN, WGM, WGN, STAGES>() <= 160 * 1024, "tile");
+    static_assert(TM % 32 == 0 && TN % 32 == 0 && BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && NW % 2 == 0 && STAGES >= 2 && tile_lds_all<BM, BN, WGM, WGN, STAGES>() <= 160 * 1024, "tile");
 
     extern __shared__ __attribute__((aligned(1024))) char tile_smem[];
     if (p.hp) __builtin_amdgcn_s_setprio(3);
@@ -138,9 +140,15 @@ __global__ void __launch_bounds__(64 * WGM * WGN, (tile_waves_per_simd<BM, BN, W
     place_tile(a.order, xcd_range(a.order.tiles, blockIdx.x), tm, tn);
     const int m0 = tm * BM, n0 = tn * BN;
 
+    // the channels' scales and biases lie behind the ring (zeros past the end)
+    float* const channels = (float*)(tile_smem + tile_lds<BM, BN, WGM, WGN, STAGES>());
+    for (int i = tid; i < BN; i += NT) {
+        channels[i] = n0 + i < p.N ? p.ws[n0 + i] : 0.f;
+        channels[BN + i] = p.bias && n0 + i < p.N ? p.bias[n0 + i] : 0.f;
+    }
     // a residual's part of the epilogue: LANES lanes lie along a row, 8 outputs each; on tiles of 32 rows to a wavefront all of it is requested ahead of the first slice
     constexpr int LANES = BN / 8, ROWS = WGM * 32 / (NT / LANES);      // rows of a lane among 32 of each wavefront
-    const int c0 = tid % LANES * 8, n = n0 + c0, many = p.N - n < 8 ? p.N - n : 8;
+    const int c0 = tid % LANES * 8, n = n0 + c0, many = p.N - n;
     half8 res[ROWS];
     auto row_of = [&](int b, int i) __attribute__((always_inline)) {
         const int r = i * (NT / LANES) + tid / LANES;
@@ -152,13 +160,7 @@ __global__ void __launch_bounds__(64 * WGM * WGN, (tile_waves_per_simd<BM, BN, W
             const int m = row_of(b, i);
 #pragma unroll
             for (int j = 0; j < 8; ++j) res[i][j] = (half_t)0.f;
-            if (!p.res || m >= p.M) continue;
-            const half_t* at = p.res + (long long)m * p.N + n;
-            if (many == 8) res[i] = ((const AnyHalf8*)at)->h;
-            else
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (j < many) res[i][j] = at[j];
+            if (p.res && m < p.M && many >= 8) res[i] = ((const AnyHalf8*)(p.res + (long long)m * p.N + n))->h;
         }
     };
     if (TMB == 1) load_res(0);
@@ -224,8 +226,10 @@ __global__ void __launch_bounds__(64 * WGM * WGN, (tile_waves_per_simd<BM, BN, W
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");   // the zeros past the end have arrived: LDS is free
 
-    // ---- epilogue: a lane holds the sums of y[m][n .. n + 3], n at 8 g + 4 lh.  Rows of the result begin at any multiple of its element (N may be odd): 16 bytes at a time
+    // ---- epilogue, one for each activation: a lane holds the sums of y[m][n .. n + 3], n at 8 g + 4 lh.  Rows of the result begin at any multiple of its element (N may be odd): 16 bytes at a time
     // all the same, which the memory takes at any address.
+    auto epilogue = [&](auto activation) __attribute__((always_inline)) {
+    constexpr int ACT = decltype(activation)::value;
     if (!p.out_f32 && !p.res) {
         // rounded results leave through LDS
         half_t* const out = (half_t*)tile_smem;
@@ -238,12 +242,10 @@ __global__ void __launch_bounds__(64 * WGM * WGN, (tile_waves_per_simd<BM, BN, W
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
                     const int nt = wn0 + t * 32 + 8 * g + 4 * lh;
+                    const floatx4 ws = *(const floatx4*)(channels + nt), bias = *(const floatx4*)(channels + BN + nt);
                     half4 h;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int n = n0 + nt + j < p.N ? n0 + nt + j : p.N - 1;
-                        h[j] = (half_t)finish(acc[t][b][4 * g + j], xs, p.ws[n], p.bias ? p.bias[n] : 0.f, 0.f, p.act);
-                    }
+                    for (int j = 0; j < 4; ++j) h[j] = (half_t)finish(acc[t][b][4 * g + j], xs, ws[j], bias[j], 0.f, ACT);
                     *(half4*)(out + mt * LDC + nt) = h;
                 }
         }
@@ -255,6 +257,7 @@ __global__ void __launch_bounds__(64 * WGM * WGN, (tile_waves_per_simd<BM, BN, W
             const half8 h = *(const half8*)(out + r * LDC + c);
             if (n + 8 <= p.N) *(AnyHalf8*)y = AnyHalf8{h};
             else
+#pragma unroll 1
                 for (int j = 0; j < p.N - n; ++j) y[j] = out[r * LDC + c + j];
         }
         return;
@@ -263,15 +266,9 @@ __global__ void __launch_bounds__(64 * WGM * WGN, (tile_waves_per_simd<BM, BN, W
     int* const sums = (int*)tile_smem;
     constexpr int LDS_N = BN + 4;
     static_assert(WGM * 32 * LDS_N * 4 <= (int)tile_lds<BM, BN, WGM, WGN, STAGES>() && WGM * 32 % (NT / LANES) == 0, "staging");
-    float ws[8], bias[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const int c = n + j < p.N ? n + j : p.N - 1;
-        ws[j] = p.ws[c];
-        bias[j] = p.bias ? p.bias[c] : 0.f;
-    }
 #pragma unroll
     for (int b = 0; b < TMB; ++b) {
+        __builtin_amdgcn_sched_barrier(0);             // (nothing of the next 32 rows ahead of these: there are no registers for it)
         float xs[ROWS];
 #pragma unroll
         for (int i = 0; i < ROWS; ++i) xs[i] = row_of(b, i) < p.M ? p.xs[row_of(b, i)] : 0.f;
@@ -287,32 +284,41 @@ __global__ void __launch_bounds__(64 * WGM * WGN, (tile_waves_per_simd<BM, BN, W
         for (int i = 0; i < ROWS; ++i) {
             const int* from = sums + (i * (NT / LANES) + tid / LANES) * LDS_N + c0;
             const intx4 lo = *(const intx4*)from, hi = *(const intx4*)(from + 4);
-            float y[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] = finish(j < 4 ? lo[j] : hi[j - 4], xs[i], ws[j], bias[j], (float)res[i][j], p.act);
             const int m = row_of(b, i);
             if (m >= p.M || many <= 0) continue;
             const long long at = (long long)m * p.N + n;
-            if (p.out_f32) {
-                if (many == 8) {
-                    *(AnyFloat4*)((float*)p.y + at) = AnyFloat4{floatx4{y[0], y[1], y[2], y[3]}};
-                    *(AnyFloat4*)((float*)p.y + at + 4) = AnyFloat4{floatx4{y[4], y[5], y[6], y[7]}};
-                } else
+            if (many < 8) {                            // the last channels
+#pragma unroll 1
+                for (int j = 0; j < many; ++j) {
+                    const float y = finish(from[j], xs[i], channels[c0 + j], channels[BN + c0 + j], p.res ? (float)p.res[at + j] : 0.f, ACT);
+                    if (p.out_f32) ((float*)p.y)[at + j] = y;
+                    else ((half_t*)p.y)[at + j] = (half_t)y;
+                }
+                continue;
+            }
+            floatx4 y[2];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (j < many) ((float*)p.y)[at + j] = y[j];
+            for (int k = 0; k < 2; ++k) {
+                const floatx4 ws = *(const floatx4*)(channels + c0 + 4 * k), bias = *(const floatx4*)(channels + BN + c0 + 4 * k);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) y[k][j] = finish((k ? hi : lo)[j], xs[i], ws[j], bias[j], (float)res[i][4 * k + j], ACT);
+            }
+            if (p.out_f32) {
+                *(AnyFloat4*)((float*)p.y + at) = AnyFloat4{y[0]};
+                *(AnyFloat4*)((float*)p.y + at + 4) = AnyFloat4{y[1]};
             } else {
                 half8 h;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) h[j] = (half_t)y[j];
-                if (many == 8) *(AnyHalf8*)((half_t*)p.y + at) = AnyHalf8{h};
-                else
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (j < many) ((half_t*)p.y)[at + j] = h[j];
+                for (int j = 0; j < 8; ++j) h[j] = (half_t)y[j >> 2][j & 3];
+                *(AnyHalf8*)((half_t*)p.y + at) = AnyHalf8{h};
             }
         }
     }
+    };
+    if (p.act == ACT_GELU) epilogue(std::integral_constant<int, ACT_GELU>{});
+    else if (p.act == ACT_RELU) epilogue(std::integral_constant<int, ACT_RELU>{});
+    else if (p.act == ACT_RELU6) epilogue(std::integral_constant<int, ACT_RELU6>{});
+    else epilogue(std::integral_constant<int, ACT_NONE>{});
 }
 
 template <int BM, int BN, int WGM, int WGN, int STAGES>
@@ -322,7 +328,7 @@ static int launch_tile(const GemmI8& p, hipStream_t stream) {
     ConvParams order{};
     set_tile_order(order, tiles_m, (int)tiles_n, BM, BN, SLICE, 1);
     const TileArgs a{p, order.order};
-    constexpr unsigned lds = tile_lds<BM, BN, WGM, WGN, STAGES>();
+    constexpr unsigned lds = tile_lds_all<BM, BN, WGM, WGN, STAGES>();
     auto kernel = gemm_i8_tile_kernel<BM, BN, WGM, WGN, STAGES>;
     static std::atomic<bool> configured{false};        // (per tile; setting the attribute twice is harmless)
     if (lds > 64 * 1024 && !configured.load(std::memory_order_acquire)) {

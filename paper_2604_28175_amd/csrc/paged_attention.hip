@@ -131,14 +131,15 @@ struct RawBlock {
     static constexpr int KP = D * (I8 ? 1 : 2) / 64, VW = D / 16 * (I8 ? 1 : 2) / 4;       // pieces of a key per lane; words of a value
     uintx4 k[2][KP];
     unsigned v[8][VW];
-    __device__ __forceinline__ void load(const strait_kv_cache& c, int place, int row, int l16, int g4) {
-        const long long at = ((long long)place * c.page_tokens + row) * (D * (I8 ? 1 : 2));
-        const char* kp = (const char*)c.k + at;
-        const char* vp = (const char*)c.v + at;
+    __device__ __forceinline__ void load_k(const strait_kv_cache& c, int place, int row, int l16, int g4) {
+        const char* kp = (const char*)c.k + ((long long)place * c.page_tokens + row) * (D * (I8 ? 1 : 2));
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
             for (int u = 0; u < KP; ++u) k[kb][u] = *(const uintx4*)(kp + (unsigned)((kb * 16 + l16) * KP * 64 + 16 * g4 + 64 * u));
+    }
+    __device__ __forceinline__ void load_v(const strait_kv_cache& c, int place, int row, int l16, int g4) {
+        const char* vp = (const char*)c.v + ((long long)place * c.page_tokens + row) * (D * (I8 ? 1 : 2));
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const char* src = vp + (unsigned)((16 * (e >> 2) + 4 * g4 + (e & 3)) * KP * 64 + l16 * VW * 4);
@@ -152,6 +153,7 @@ struct RawBlock {
 template <int D, bool I8, int RT>
 __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_stream_kernel(const PagedArgs a) {
     constexpr int J = D / 16, LDO = D + 4;
+    constexpr bool AHEAD = D == 64 || I8 || RT == 1;   // registers for a whole block beside the one that is worked on (two rows' tiles of fp16: the next keys where these are done with)
     __shared__ float so[2][RT * 16][LDO];
     __shared__ float sml[2][RT * 16][2];
     const PagedAttention& p = a.p;
@@ -194,7 +196,8 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_stream_kernel(const
     // whether a row sees the key `off` behind some key of which it is `past` tokens past and which is `sinks` keys in front of the last sink
     const int window = p.window ? p.window : 0x7fffffff;
     auto sees = [&](int off, int past, int sinks) __attribute__((always_inline)) { return off <= past && (off > past - window || off < sinks); };
-    auto work = [&](const RawBlock<D, I8>& raw, int k0, float kc, float vs, bool mask) __attribute__((always_inline)) {
+    // keys_done, values_done: when the registers of a block's keys and values are free
+    auto work = [&](const RawBlock<D, I8>& raw, int k0, float kc, float vs, bool mask, auto keys_done, auto values_done) __attribute__((always_inline)) {
         half8 kf[2][D / 32];
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
@@ -250,6 +253,7 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_stream_kernel(const
                 pf[x][e] = (half_t)v;
             }
         }
+        keys_done();
         unsigned w[8][RawBlock<D, I8>::VW];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -279,6 +283,7 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_stream_kernel(const
                 } else o[x][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[x], o[x][j], 0, 0, 0);
             }
         }
+        values_done();
     };
 
     // 64 of this wavefront's blocks at a time
@@ -298,22 +303,27 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_stream_kernel(const
         if (!left) continue;
         RawBlock<D, I8> next;
         int ni = __builtin_ctzll(left);
-        auto fetch = [&]() __attribute__((always_inline)) {
-            next.load(p.cache, __builtin_amdgcn_readlane(places, ni), __builtin_amdgcn_readlane(k0s, ni) & (P - 1), l16, g4);
-        };
-        fetch();
+        auto next_k = [&]() __attribute__((always_inline)) { next.load_k(p.cache, __builtin_amdgcn_readlane(places, ni), __builtin_amdgcn_readlane(k0s, ni) & (P - 1), l16, g4); };
+        auto next_v = [&]() __attribute__((always_inline)) { next.load_v(p.cache, __builtin_amdgcn_readlane(places, ni), __builtin_amdgcn_readlane(k0s, ni) & (P - 1), l16, g4); };
+        next_k();
+        next_v();
         while (left) {
-            const RawBlock<D, I8> raw = next;
-            const int i = ni;
-            left &= left - 1;
-            if (left) {
-                ni = __builtin_ctzll(left);
-                fetch();
-            }
-            const int k0 = __builtin_amdgcn_readlane(k0s, i);
+            const int i = ni, k0 = __builtin_amdgcn_readlane(k0s, i);
             const float kc = I8 ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, kcs), i)) : c;
             const float vs = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, vss), i));
-            work(raw, k0, kc, vs, !(k0 + KEYS - 1 <= t.lo && (!p.window || t.hi - k0 < p.window || k0 + KEYS - 1 < p.sinks)));
+            const bool mask = !(k0 + KEYS - 1 <= t.lo && (!p.window || t.hi - k0 < p.window || k0 + KEYS - 1 < p.sinks));
+            left &= left - 1;
+            if (left) ni = __builtin_ctzll(left);
+            if constexpr (AHEAD) {
+                const RawBlock<D, I8> raw = next;
+                if (left) {
+                    next_k();
+                    next_v();
+                }
+                work(raw, k0, kc, vs, mask, [] {}, [] {});
+            } else {                                   // (behind the last block: that one again)
+                work(next, k0, kc, vs, mask, next_k, next_v);
+            }
         }
     }
 #pragma unroll

@@ -3,6 +3,8 @@
 Tolerances.  fp16 results are off by half a step, 2^-11 of the value (2^-25 below the normal numbers), for their own rounding; what is added is said at each
 bound.  Codes of 8-bit integers and their scales are equal bit for bit: their definition names every operation.
 """
+import gc
+
 import numpy as np
 import pytest
 
@@ -19,7 +21,10 @@ def S():
     import paper_2604_28175_amd as strait
     assert torch.cuda.is_available()
     strait.torch = torch
-    return strait
+    yield strait
+    gc.collect()                              # graphs and caches of gigabytes: other files' tests measure what memory is free
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
 
 
 def dev(S, a):
