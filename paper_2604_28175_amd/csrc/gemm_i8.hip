@@ -4,7 +4,7 @@
 //
 // The sum is an int32 of the integer MFMAs and exact in any order; the epilogue is fp32, rounded once.  Two kernels:
 //
-//   gemm_i8_stream_kernel, up to 64 rows: bound by the weights' bytes.  A workgroup of 8 wavefronts has 16 NT channels and shares the reduction
+//   gemm_i8_stream_kernel, few rows: bound by the weights' bytes.  A workgroup of 8 wavefronts has 16 NT channels and shares the reduction
 //   out in pieces of 256; weights go from memory to registers in the layout of v_mfma_i32_16x16x64_i8's operand, a piece ahead, and each byte is read
 //   once on the whole chip.  The partial sums meet in LDS as integers.
 //
@@ -38,7 +38,7 @@ __global__ void __launch_bounds__(64 * STREAM_WAVES) gemm_i8_stream_kernel(const
     __shared__ int sums[16 * MT][16 * NT + 1];          // (+ 1: 16 rows at one channel lie in 16 banks)
     if (p.hp) __builtin_amdgcn_s_setprio(3);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l16 = lane & 15, g4 = lane >> 4;
-    const int n0 = (int)blockIdx.x * 16 * NT, m0 = (int)blockIdx.y * 16 * MT;
+    const int n0 = (int)blockIdx.x * 16 * NT;
     constexpr int PIECE = 64 * STREAM_STEPS;
     const int pieces = (p.K + PIECE - 1) / PIECE;
     const int8_t* wr[NT];
@@ -46,7 +46,7 @@ __global__ void __launch_bounds__(64 * STREAM_WAVES) gemm_i8_stream_kernel(const
 #pragma unroll
     for (int t = 0; t < NT; ++t) wr[t] = p.w + (long long)(n0 + 16 * t + l16 < p.N ? n0 + 16 * t + l16 : p.N - 1) * p.K;    // (rows past the end: the last one, not stored)
 #pragma unroll
-    for (int t = 0; t < MT; ++t) xr[t] = p.x + (long long)(m0 + 16 * t + l16 < p.M ? m0 + 16 * t + l16 : p.M - 1) * p.K;
+    for (int t = 0; t < MT; ++t) xr[t] = p.x + (long long)(16 * t + l16 < p.M ? 16 * t + l16 : p.M - 1) * p.K;
     auto at = [&](const int8_t* row, int piece, int s) __attribute__((always_inline)) {
         const int k = piece * PIECE + 64 * s + 16 * g4;
         return k < p.K ? *(const intx4*)(row + k) : intx4{0, 0, 0, 0};
@@ -94,10 +94,10 @@ __global__ void __launch_bounds__(64 * STREAM_WAVES) gemm_i8_stream_kernel(const
     }
     __syncthreads();
     for (int i = threadIdx.x; i < 256 * MT * NT; i += 64 * STREAM_WAVES) {
-        const int r = i / (16 * NT), c = i - r * (16 * NT), m = m0 + r, n = n0 + c;
+        const int m = i / (16 * NT), c = i - m * (16 * NT), n = n0 + c;
         if (m >= p.M || n >= p.N) continue;
         const long long o = (long long)m * p.N + n;
-        const float y = finish(sums[r][c], p.xs[m], p.ws[n], p.bias ? p.bias[n] : 0.f, p.res ? (float)p.res[o] : 0.f, p.act);
+        const float y = finish(sums[m][c], p.xs[m], p.ws[n], p.bias ? p.bias[n] : 0.f, p.res ? (float)p.res[o] : 0.f, p.act);
         if (p.out_f32) ((float*)p.y)[o] = y;
         else ((half_t*)p.y)[o] = (half_t)y;
     }
@@ -341,23 +341,26 @@ static int launch_tile(const GemmI8& p, hipStream_t stream) {
 }
 template <int MT, int NT, int STEPS>
 static void launch_stream(const GemmI8& p, hipStream_t stream) {
-    hipLaunchKernelGGL((gemm_i8_stream_kernel<MT, NT, STEPS>), dim3((unsigned)((p.N + 16LL * NT - 1) / (16 * NT)), (unsigned)((p.M + 16 * MT - 1) / (16 * MT))), dim3(64 * STREAM_WAVES), 0, stream, p);
+    hipLaunchKernelGGL((gemm_i8_stream_kernel<MT, NT, STEPS>), dim3((unsigned)((p.N + 16LL * NT - 1) / (16 * NT))), dim3(64 * STREAM_WAVES), 0, stream, p);
 }
 
-// Up to 64 rows: 16 NT channels to a workgroup, NT so that there are 256 workgroups where the channels allow it (16384 x 4096 at 48 rows, NT = 4, 2, 1: 18.1, 22.6 and 39.6 us; 4096 x
-// 4096: 16.8, 12.5 and 11.7), pieces of 64, 128 or 256 as the registers allow.
-// More: the tile with the least time for the most tiles that a compute unit gets.  A slice of 128 takes a unit 0.25 us on a 64 x 64 tile, 0.70 on 128 x 128, 1.23 on 256 x 128
-// and 2.42 on 256 x 256 with all units at work (256 x 4096 x 4096 12.7, 20.4, 31.5 and 55.9 us; 2048 x 4096 x 4096 70, 51.6, 43.4 and 60.2; 8192 x 16384 x 4096 1205, 862, 683 and 623).
+// Up to 16 rows, and up to 48 where 16 channels to a workgroup are one round of workgroups: the stream, 16 NT channels to a workgroup, NT so that there are 256 workgroups where the channels
+// allow it (16384 x 4096 at 16 rows, NT = 4: 13.0 us; a tile 13.5; 4096 x 4096 7.0 and 10.7), pieces of 128 or 256 as the registers allow.  Every workgroup of it reads all of x, so the
+// tile's 64 channels win from there on: 17 x 12288 x 4096 16.3 and 11.3 us, 32 x 16384 x 4096 15.4 and 13.6, 48 x 4096 x 4096 11.8 and 10.9, 64 x 4096 x 16384 38.6 and 29.8; for the stream still
+// 32 x 4096 x 4096 8.9 and 10.8, 33 x 4096 x 2048 6.0 and 7.0, 33 x 2304 x 1024 4.4 and 5.3.
+// More: the tile with the least time for the most tiles that a compute unit gets.  A slice of 128 takes a unit 0.24 us on a 64 x 64 tile, 0.66 on 128 x 128, 1.11 on 256 x 128
+// and 2.05 on 256 x 256 with all units at work (256 x 4096 x 4096 12.0, 17.9, 27.0 and 45.1 us; 512 x 5120 x 2048 16.5, 12.8, 17.9 and 28.0; 2048 x 4096 x 4096 62.7, 45.7, 38.3 and 49.6;
+// 4096 x 4096 x 4096 119, 88.2, 75.6 and 68.2; 8192 x 16384 x 4096 1191, 777, 615 and 529).
 int launch_gemm_i8(const GemmI8& p, hipStream_t stream) {
     int rc = 0;
-    if (p.M <= 64) {
-        const int nt = p.N >= 16384 ? 4 : p.N >= 8192 ? 2 : 1;
-        if (p.M <= 16) nt == 4 ? launch_stream<1, 4, 2>(p, stream) : nt == 2 ? launch_stream<1, 2, 4>(p, stream) : launch_stream<1, 1, 4>(p, stream);
-        else if (p.M <= 32) nt == 4 ? launch_stream<2, 4, 2>(p, stream) : nt == 2 ? launch_stream<2, 2, 2>(p, stream) : launch_stream<2, 1, 4>(p, stream);
-        else if (p.M <= 48) nt == 4 ? launch_stream<3, 4, 1>(p, stream) : nt == 2 ? launch_stream<3, 2, 2>(p, stream) : launch_stream<3, 1, 4>(p, stream);
-        else nt == 4 ? launch_stream<4, 4, 1>(p, stream) : nt == 2 ? launch_stream<4, 2, 2>(p, stream) : launch_stream<4, 1, 2>(p, stream);
+    if (p.M <= 16) {
+        p.N >= 16384 ? launch_stream<1, 4, 2>(p, stream) : p.N >= 8192 ? launch_stream<1, 2, 4>(p, stream) : launch_stream<1, 1, 4>(p, stream);
+    } else if (p.M <= 32 && p.N <= 4096) {
+        launch_stream<2, 1, 4>(p, stream);
+    } else if (p.M <= 48 && p.N <= 4096 && p.K <= 2048) {
+        launch_stream<3, 1, 4>(p, stream);
     } else {
-        const struct { int bm, bn; float us; } tile[4] = {{64, 64, 0.25f}, {128, 128, 0.70f}, {256, 128, 1.23f}, {256, 256, 2.42f}};
+        const struct { int bm, bn; float us; } tile[4] = {{64, 64, 0.24f}, {128, 128, 0.66f}, {256, 128, 1.11f}, {256, 256, 2.05f}};
         int best = 0;
         float least = 0.f;
         for (int i = 0; i < 4; ++i) {
