@@ -386,8 +386,8 @@ strait_status strait_k_argmax_f16(void* stream, const void* x, int32_t rows, int
 
 /* ---- operators of a decoder that answers token by token: device pointers + stream ---------------
  * Like the entry points above: asynchronous on `stream`, whose device must be the current one; nothing is allocated, so all of them may be
- * captured into a graph.  Activations fp16.  What host arguments say is checked (E_INVALID, E_SHAPE); what lies in device memory (lengths, page
- * numbers) is held inside the bounds that the host arguments give, as each entry says. */
+ * captured into a graph.  Activations fp16.  What host arguments say is checked (E_INVALID; E_SHAPE, also for launches of
+ * 2^32 threads and more); what lies in device memory (lengths, page numbers) is held inside the bounds that the host arguments give, as each entry says. */
 
 /* Rows of activations as 8-bit integers with one scale each: s = max |x| * (1 / 127), q = x * (1 / s) rounded to the nearest, ties to even (all in fp32; 0 where s
  * is 0).  x [M] rows of K fp16, `pitch` elements from one to the next (a multiple of 8, >= K; columns of a wider tensor will do); q int8 [M][K]; scale fp32 [M].
@@ -396,14 +396,14 @@ strait_status strait_k_argmax_f16(void* stream, const void* x, int32_t rows, int
 strait_status strait_k_quantize_rows(void* stream, const void* x, int32_t M, int32_t K, int64_t pitch, int8_t* q, float* scale, int32_t hp);
 /* Y[M,N] = act(xs[m] ws[n] sum_k x[m,k] w[n,k] + bias[n] (+ res[m,n])): a product in 8-bit integers with a scale for each token (row of x int8 [M][K]) and
  * each output channel (row of w int8 [N][K]).  The sum is exact (int32), the rest fp32, rounded once; bias fp32 [N] or NULL, res fp16 [M][N] or NULL,
- * y fp16 [M][N] (fp32 when out_f32 != 0); y may be res.  K a multiple of 16 up to 131056 (E_SHAPE: beyond, 128 * 128 * K leaves int32); x and w 16-byte aligned, res and y by
+ * y fp16 [M][N] (fp32 when out_f32 != 0); y may be res where it is fp16.  K a multiple of 16 up to 131056 (E_SHAPE: beyond, 128 * 128 * K leaves int32); x and w 16-byte aligned, res and y by
  * their element.  M = 0 does nothing.  All bits are the same whatever M a row is part of. */
 strait_status strait_k_gemm_i8(void* stream, const int8_t* x, const float* x_scale, const int8_t* w, const float* w_scale, const float* bias,
                                int32_t M, int32_t N, int32_t K, int32_t act, const void* res, void* y, int32_t out_f32, int32_t hp);
 
 /* A paged cache of keys and values: k, v [pages][kv_heads][page_tokens][head_dim], 16-byte aligned.  STRAIT_KV_F16: fp16 (the scales are not
- * looked at).  STRAIT_KV_I8: int8 codes, k_scale, v_scale fp32 [pages][kv_heads]; a code stands for code * scale of its page and head, scales >= 0.
- * page_tokens 32, 64, 128 or 256; head_dim 64 or 128 (E_SHAPE otherwise).  Neither has to be initialised. */
+ * looked at).  STRAIT_KV_I8: int8 codes, k_scale, v_scale fp32 [pages][kv_heads]; a code stands for code * scale of its page and head, scales 0 to 4096 (fp16 numbers
+ * have 516 at most).  page_tokens 32, 64, 128 or 256; head_dim 64 or 128 (E_SHAPE otherwise).  Neither has to be initialised. */
 typedef enum { STRAIT_KV_F16 = 0, STRAIT_KV_I8 = 1 } strait_kv_type;
 typedef struct strait_kv_cache {
     void* k;
@@ -416,7 +416,7 @@ typedef struct strait_kv_cache {
  * none is allowed), and kv_len[b] (int32 [seqs]) tokens of it are in the cache, those of this step included: its i-th of n new tokens is at
  * position p = kv_len[b] - n + i, which is row p % page_tokens of page page_table[b * table_pitch + p / page_tokens] (int32).
  * max_q: at least the most tokens that a sequence brings; max_kv: at least the longest kv_len (host: they size the launches; 1 <= max_q <= tokens, ceil(max_kv /
- * page_tokens) <= table_pitch, E_INVALID otherwise).  A sequence's tokens from the max_q-th on, and those outside every sequence, are left out: nothing is
+ * page_tokens) <= table_pitch, E_INVALID otherwise; max_kv up to 2^29, E_SHAPE).  A sequence's tokens from the max_q-th on, and those outside every sequence, are left out: nothing is
  * written for them.  A kv_len outside 0 .. max_kv counts as the nearer of the two.  Page numbers outside 0 .. pages - 1 are not followed.
  * tokens = 0 does nothing. */
 typedef struct strait_kv_batch {
@@ -443,7 +443,7 @@ strait_status strait_rope_table(float* table, int32_t positions, int32_t dim, do
 strait_status strait_k_kv_append(void* stream, const strait_kv_cache* cache, const strait_kv_batch* batch, const void* q, const void* k, const void* v,
                                  int64_t pitch_q, int64_t pitch_k, int64_t pitch_v, int32_t heads, const float* rope, int32_t rope_rows, int32_t rope_dim,
                                  int32_t interleaved, void* q_out, int32_t hp);
-/* Attention of a step's tokens over the cache, which holds them already.  q fp16: row t at t * pitch_q, [heads][head_dim]; out fp16 [tokens][heads][head_dim]; heads a
+/* Attention of a step's tokens over the cache, which holds them already.  q fp16: row t at t * pitch_q, [heads][head_dim]; out fp16 [tokens][heads][head_dim], apart from q; heads a
  * multiple of kv_heads, head h reads kv head h / (heads / kv_heads).  The token at position p sees key j where
  *     j <= p  and  (window == 0  or  p - j < window  or  j < sinks),
  * out = sum_j softmax_j(scale q . k_j) v_j over what it sees; a token that sees nothing (at a negative position) gets zeros.  Keys on pages that are not followed count as not seen,

@@ -30,6 +30,7 @@ int check_batch(const char* what, const strait_kv_cache* c, const strait_kv_batc
     if (!b->q_start || !b->kv_len || !b->page_table) return invalid(what, "null q_start, kv_len or page_table");
     if (b->max_q < 1 || b->max_q > b->tokens || b->max_kv < 1) return invalid(what, "needs 1 <= max_q <= tokens and max_kv >= 1");
     if (b->table_pitch < (b->max_kv + (long long)c->page_tokens - 1) / c->page_tokens) return invalid(what, "table_pitch is too small for max_kv");
+    if (b->max_kv > 1 << 29) return shape(what, "max_kv is 2^29 at most");
     return STRAIT_OK;
 }
 int check_rows(const char* what, const void* p, int64_t pitch, long long width, const char* why) {
@@ -78,6 +79,7 @@ strait_status strait_k_gemm_i8(void* stream, const int8_t* x, const float* x_sca
     if (K % 16 || K > 131056) return shape(what, "K must be a multiple of 16 up to 131056");
     if (act < STRAIT_ACT_NONE || act > STRAIT_ACT_GELU) return invalid(what, "unknown activation");
     if (M == 0) return STRAIT_OK;
+    if (res && out_f32 && res == y) return invalid(what, "y may be res only where both are fp16");
     if (!x || !x_scale || !w || !w_scale || !y || !aligned16(x) || !aligned16(w)) return invalid(what, "null or misaligned operands");
     if (reinterpret_cast<uintptr_t>(y) % (out_f32 ? 4 : 2) || reinterpret_cast<uintptr_t>(res) % 2 || reinterpret_cast<uintptr_t>(x_scale) % 4 ||
         reinterpret_cast<uintptr_t>(w_scale) % 4 || reinterpret_cast<uintptr_t>(bias) % 4) return invalid(what, "misaligned operands");

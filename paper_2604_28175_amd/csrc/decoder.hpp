@@ -7,6 +7,8 @@ namespace strait {
 
 int launch_quantize_rows(const half_t* x, int M, int K, long long pitch, int8_t* q, float* scale, int hp, hipStream_t stream);
 
+constexpr long long MOST_WORKGROUPS = 0xffffff;        // of 256 threads: a launch has less than 2^32 of these
+
 struct GemmI8 {
     const int8_t* x; const float* xs;
     const int8_t* w; const float* ws;

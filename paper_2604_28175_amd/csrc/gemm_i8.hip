@@ -324,7 +324,7 @@ __global__ void __launch_bounds__(64 * WGM * WGN, (tile_waves_per_simd<BM, BN, W
 template <int BM, int BN, int WGM, int WGN, int STAGES>
 static int launch_tile(const GemmI8& p, hipStream_t stream) {
     const long long tiles_m = (p.M + BM - 1LL) / BM, tiles_n = (p.N + BN - 1LL) / BN;
-    if (tiles_m * tiles_n > 0x3fffffffLL) { set_error("gemm_i8: grid too large"); return STRAIT_E_SHAPE; }
+    if (tiles_m * tiles_n * (WGM * WGN / 4) > MOST_WORKGROUPS) { set_error("gemm_i8: grid too large"); return STRAIT_E_SHAPE; }
     ConvParams order{};
     set_tile_order(order, tiles_m, (int)tiles_n, BM, BN, SLICE, 1);
     const TileArgs a{p, order.order};
@@ -340,8 +340,11 @@ static int launch_tile(const GemmI8& p, hipStream_t stream) {
     return 0;
 }
 template <int MT, int NT, int STEPS>
-static void launch_stream(const GemmI8& p, hipStream_t stream) {
-    hipLaunchKernelGGL((gemm_i8_stream_kernel<MT, NT, STEPS>), dim3((unsigned)((p.N + 16LL * NT - 1) / (16 * NT))), dim3(64 * STREAM_WAVES), 0, stream, p);
+static int launch_stream(const GemmI8& p, hipStream_t stream) {
+    const long long groups = (p.N + 16LL * NT - 1) / (16 * NT);
+    if (groups * (STREAM_WAVES / 4) > MOST_WORKGROUPS) { set_error("gemm_i8: grid too large"); return STRAIT_E_SHAPE; }
+    hipLaunchKernelGGL((gemm_i8_stream_kernel<MT, NT, STEPS>), dim3((unsigned)groups), dim3(64 * STREAM_WAVES), 0, stream, p);
+    return 0;
 }
 
 // Up to 16 rows, and up to 48 where 16 channels to a workgroup are one round of workgroups: the stream, 16 NT channels to a workgroup, NT so that there are 256 workgroups where the channels
@@ -354,11 +357,11 @@ static void launch_stream(const GemmI8& p, hipStream_t stream) {
 int launch_gemm_i8(const GemmI8& p, hipStream_t stream) {
     int rc = 0;
     if (p.M <= 16) {
-        p.N >= 16384 ? launch_stream<1, 4, 2>(p, stream) : p.N >= 8192 ? launch_stream<1, 2, 4>(p, stream) : launch_stream<1, 1, 4>(p, stream);
+        rc = p.N >= 16384 ? launch_stream<1, 4, 2>(p, stream) : p.N >= 8192 ? launch_stream<1, 2, 4>(p, stream) : launch_stream<1, 1, 4>(p, stream);
     } else if (p.M <= 32 && p.N <= 4096) {
-        launch_stream<2, 1, 4>(p, stream);
+        rc = launch_stream<2, 1, 4>(p, stream);
     } else if (p.M <= 48 && p.N <= 4096 && p.K <= 2048) {
-        launch_stream<3, 1, 4>(p, stream);
+        rc = launch_stream<3, 1, 4>(p, stream);
     } else {
         const struct { int bm, bn; float us; } tile[4] = {{64, 64, 0.24f}, {128, 128, 0.66f}, {256, 128, 1.11f}, {256, 256, 2.05f}};
         int best = 0;

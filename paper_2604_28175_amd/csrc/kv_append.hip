@@ -221,7 +221,9 @@ __global__ void __launch_bounds__(256) kv_append_kernel(const KvAppend p, const 
         const int what = c < nq ? 0 : c < nq + nkv ? 1 : 2, r = what == 0 ? c : what == 1 ? c - nq : c - nq - nkv, h = r >> shift, d = (r & (per - 1)) * 8;
         const half_t* x = what == 0 ? p.q + t * p.pitch_q : what == 1 ? p.k + t * p.pitch_k : p.v + t * p.pitch_v;
         half_t* at = what == 0 ? p.q_out + ((long long)t * p.heads + h) * D : (half_t*)(what == 1 ? p.cache.k : p.cache.v) + (row0 + (long long)h * P) * D;
-        store_half8(at + d, rotated<false>(x + h * D, d, what == 2 ? nullptr : rope, p.rope_dim, p.interleaved));
+        const Eight e = rotated<false>(x + h * D, d, what == 2 ? nullptr : rope, p.rope_dim, p.interleaved);
+        __builtin_amdgcn_wave_barrier();               // (q_out may be q: a wavefront has whole heads, and both halves of its pairs before it stores)
+        store_half8(at + d, e);
     }
 }
 
@@ -237,7 +239,7 @@ int launch_kv_append(const KvAppend& p, hipStream_t stream) {
         const long long each = (p.batch.max_q + P - 2) / P + 1, direct = each * p.batch.seqs, counted = p.batch.tokens / P + 2LL * p.batch.seqs;
         if (direct <= counted) { g.pages_each = (int)each; g.by_pages_each = divisor(each); }
         const long long items = (direct <= counted ? direct : counted) * p.cache.kv_heads * 2;
-        if (items > 0x3fffffffLL) { set_error("kv_append: grid too large"); return STRAIT_E_SHAPE; }
+        if (items > MOST_WORKGROUPS) { set_error("kv_append: grid too large"); return STRAIT_E_SHAPE; }
         g.items = (int)items;
         g.blocks = waves ? (g.items + 3) / 4 : g.items;
     }
@@ -245,6 +247,7 @@ int launch_kv_append(const KvAppend& p, hipStream_t stream) {
     // 25.9, 128 of 512 7.6 and 4.4)
     g.token_threads = p.batch.tokens >= 2048 && (p.heads + (i8 ? 0 : 2 * p.cache.kv_heads)) * p.cache.head_dim / 8 < 512 ? 64 : 256;
     const long long tokens = i8 && !p.heads ? 0 : g.token_threads == 64 ? (p.batch.tokens + 3) / 4 : p.batch.tokens;
+    if (g.blocks + tokens > MOST_WORKGROUPS) { set_error("kv_append: grid too large"); return STRAIT_E_SHAPE; }
     const dim3 grid((unsigned)(g.blocks + tokens)), block(256);
     if (!i8) hipLaunchKernelGGL((kv_append_kernel<false, 256, 1>), grid, block, 0, stream, p, g);
     else if (pieces <= 64) hipLaunchKernelGGL((kv_append_kernel<true, 64, 1>), grid, block, 0, stream, p, g);

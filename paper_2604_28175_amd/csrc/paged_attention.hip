@@ -28,6 +28,8 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
 
 constexpr int KEYS = 32;                 // of a block
+constexpr int NOWHERE = 0x30000000;      // a key behind all others (max_kv is 2^29 at most), and
+constexpr int NO_WINDOW = 0x3fffffff;    // a window that holds every key: differences of positions, these and sinks stay in 32 bits
 constexpr int PAGED_WAVES = 4;
 
 // Bytes e and e + 1 of a word of codes (biased by 128) as fp16: 0x6400 + byte is 1024 + byte, from which one fused multiply-add takes 1152 and makes any power of two's multiple
@@ -70,9 +72,9 @@ struct PagedArgs {
     int tiles, rows;                     // tiles of a sequence's rows and head, rows of a tile
     int items;                           // (sequence, tile) pairs that are found by counting; 0: each sequence has `tiles`
     int per_part, parts;                 // blocks of a part, parts at most
-    int join_tokens;                     // of each sequence that the join looks at; 0: it finds each token's sequence
+    int join_tokens;                     // of each sequence that the join looks at; 0: all tokens, of which it finds the sequences
     int slots;                           // parts of a row that the workspace has room for
-    float* o; float* ml;                 // of parts: [tokens heads][slots][D] and [..][2]: the output over the sum, the maximum and the sum
+    float* o; float* ml;                 // of parts: [joined tokens][heads][slots][D] and [..][2]: the output over the sum, the maximum and the sum
     Divisor by_group, by_heads, by_seqs, by_tiles, by_items, by_q_heads, by_join;
 };
 
@@ -81,6 +83,11 @@ struct Tile { int r0, lo, hi; bool any; };
 __device__ __forceinline__ Tile tile_of(const PagedArgs& a, const Sequence& s, int tile) {
     const int r0 = tile * a.rows, last = divide(r0 + a.rows - 1, a.by_group), rows = s.n * a.group;
     return {r0, s.past + divide(r0, a.by_group), s.past + (last < s.n ? last : s.n - 1), r0 < rows && rows > a.from && rows <= a.to};
+}
+
+// Where the parts of a sequence's i-th token lie: joined tokens are numbered by sequence, or as they come.
+__device__ __forceinline__ long long joined_token(const PagedArgs& a, int b, const Sequence& s, int i) {
+    return a.join_tokens ? (long long)b * a.join_tokens + i : s.first + i;
 }
 
 // Workgroup ((part tiles + tile) seqs + b') heads + h: every sequence's first part comes before any second one, a sequence's last tile, which sees the most keys, before the others,
@@ -194,7 +201,7 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_stream_kernel(const
     const float c = p.scale * 1.44269504088896340736f * (I8 ? 512.f : 1.f);
 
     // whether a row sees the key `off` behind some key of which it is `past` tokens past and which is `sinks` keys in front of the last sink
-    const int window = p.window ? p.window : 0x7fffffff;
+    const int window = p.window ? p.window : NO_WINDOW;
     auto sees = [&](int off, int past, int sinks) __attribute__((always_inline)) { return off <= past && (off > past - window || off < sinks); };
     // keys_done, values_done: when the registers of a block's keys and values are free
     auto work = [&](const RawBlock<D, I8>& raw, int k0, float kc, float vs, bool mask, auto keys_done, auto values_done) __attribute__((always_inline)) {
@@ -374,9 +381,8 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_stream_kernel(const
     for (int x = 0; x < RT; ++x) {
         if (token[x] < 0) continue;
         const float inv = l[x] == 0.f ? 0.f : 1.f / l[x];      // nothing seen: zeros
-        const long long row = (long long)token[x] * p.heads + head[x];
         if (whole) {
-            half_t* out = p.out + row * D;
+            half_t* out = p.out + ((long long)token[x] * p.heads + head[x]) * D;
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
                 half_t y[J];
@@ -386,7 +392,7 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_stream_kernel(const
                 else *(uint2*)(out + J * (4 * g4 + v)) = *(const uint2*)y;
             }
         } else {
-            const long long slot = row * a.slots + part;
+            const long long slot = (joined_token(a, b, s, token[x] - s.first) * p.heads + head[x]) * a.slots + part;
             float* out = a.o + slot * D;
 #pragma unroll
             for (int v = 0; v < 4; ++v)
@@ -448,7 +454,7 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
 #pragma unroll
         for (int v = 0; v < 16; ++v) o[db][v] = 0.f;
     float m = -INFINITY, l = 0.f;
-    const float c = p.scale * 1.44269504088896340736f;
+    const float c = fmaxf(p.scale * 1.44269504088896340736f, 0x1p-126f);
 
     // ---- memory -> registers -> LDS.  Chunk q of 16 bytes of row r lies at q ^ (r % 16) for K (D = 64: r % 8), whose operand is 16 rows at one chunk.  V's
     // operand is 4 rows at 4 chunks at a time: the rows' bits go to the chunk's bits above those (and to the lowest, for the sake of the stores)
@@ -462,7 +468,7 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
     float kcs = c, vpow = 1.f, vlog = 0.f, vinv = 1.f;
     unsigned long long full = 0, none = 0;
     auto look_up = [&](int first) __attribute__((always_inline)) {
-        k0s = 0x7fffff00;
+        k0s = NOWHERE;
         from_lo = from_hi = 0;
         if (first + lane < end) {
             const int k0 = blocks.at(first + lane) * KEYS, page = p.batch.page_table[(long long)b * p.batch.table_pitch + k0 / P];
@@ -473,10 +479,10 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
                 from_lo = (unsigned)from;
                 from_hi = (unsigned)(from >> 32);
                 if (I8) {
-                    kcs = fmaxf(p.cache.k_scale[place], 0x1p-100f) * c;       // (a scale of 0 belongs to codes of 0; times it, minus infinity were none)
+                    kcs = fmaxf(p.cache.k_scale[place] * c, 0x1p-126f);       // (times 0, minus infinity were none)
                     // a value is code 2^f, exact in fp16, f between -24 and 5 (1152 2^f is a number of fp16 too); the rest of its scale, between 1 and 2 for scales of 2^-24 to 64, goes into
-                    // the probabilities (fp16 numbers have scales of 516 at most: 16 times 2^8)
-                    const float vs = p.cache.v_scale[place];
+                    // the probabilities (128 times 2^8 at most).  Scales below 2^-60, of which no output would show a bit, count as 0: the rest would take the probabilities out of fp32.
+                    const float vs = p.cache.v_scale[place] < 0x1p-60f ? 0.f : p.cache.v_scale[place];
                     vpow = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, vs) & 0x7f800000u);
                     vpow = vs == 0.f ? 0.f : fminf(fmaxf(vpow, 0x1p-24f), 0x1p5f);
                     const float ratio = vs == 0.f ? 1.f : vs / vpow;
@@ -536,7 +542,7 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
     auto vread = [](unsigned at) { return __builtin_amdgcn_ds_read_tr16_b64_v4f16((__attribute__((address_space(3))) fp16x4*)(uintptr_t)at); };
 
     // whether a row sees the key `off` behind some key of which it is `past` tokens past and which is `sinks` keys in front of the last sink
-    const int window = p.window ? p.window : 0x7fffffff;
+    const int window = p.window ? p.window : NO_WINDOW;
     auto sees = [&](int off, int past, int sinks) __attribute__((always_inline)) { return off <= past && (off > past - window || off < sinks); };
     auto work = [&](int n, int st, bool mask) __attribute__((always_inline)) {
         const char* ks0 = tile_lds + st * STAGE;
@@ -644,9 +650,8 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
     if (!any) return;
     const float inv = l == 0.f ? 0.f : 1.f / l;        // nothing seen: zeros
     const bool whole = blocks.count <= a.per_part;
-    const long long row = (long long)(token < 0 ? 0 : token) * p.heads + head;
     if (whole) {
-        half_t* out = p.out + row * D;
+        half_t* out = p.out + ((long long)(token < 0 ? 0 : token) * p.heads + head) * D;
         // lane holds dimensions db * 32 + 8 g + 4 lh + j of its row; after the exchange with lane ^ 32, 8 of one g
 #pragma unroll
         for (int db = 0; db < D / 32; ++db)
@@ -661,7 +666,7 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
                 if (token >= 0) *(uintx4*)(out + db * 32 + 8 * (g + lh)) = uintx4{x[0], y[0], x[1], y[1]};
             }
     } else if (token >= 0) {
-        const long long slot = row * a.slots + part;
+        const long long slot = (joined_token(a, b, s, i) * p.heads + head) * a.slots + part;
 #pragma unroll
         for (int db = 0; db < D / 32; ++db)
 #pragma unroll
@@ -699,7 +704,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const PagedArgs few, co
     const Blocks blocks = visible_blocks(t.lo, t.hi, p.window, p.sinks);
     const int parts = (blocks.count + a.per_part - 1) / a.per_part;
     if (parts <= 1) return;
-    const long long row = (long long)(s.first + i) * p.heads + hq;
+    const long long row = joined_token(a, b, s, i) * p.heads + hq;
     const float2* ml = (const float2*)a.ml + row * a.slots;
     const int group = (int)threadIdx.x / GROUP, d = (int)threadIdx.x % GROUP;
     const floatx4* o = (const floatx4*)(a.o + row * a.slots * D) + d;
@@ -735,7 +740,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const PagedArgs few, co
     half_t h[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) h[j] = (half_t)(y[j] * inv);
-    *(uint2*)(p.out + row * D + d * 4) = *(const uint2*)h;
+    *(uint2*)(p.out + ((long long)(s.first + i) * p.heads + hq) * D + d * 4) = *(const uint2*)h;
 }
 
 // How a call is launched.  Sequences with up to 16 or 32 rows of a kv head: the stream kernel, tiles of 16 or 32 rows.  More: the tile kernel, 128 rows, of which a compute unit holds
@@ -781,11 +786,12 @@ static PagedPlan paged_plan(const PagedAttention& p) {
     if (rows > few.to) plan_class(r.many, false);
     few.slots = r.many.slots = std::max(few.parts, r.many.parts);
     if (few.slots > 1) {
-        // the rows to be joined: the first few tokens of each sequence, or all where tiles were shared out too
+        // the tokens to be joined: the first few of each sequence, or all where tiles were shared out too, or where they are fewer than half as many
         few.join_tokens = r.many.parts > 1 ? 0 : (int)std::min<long long>(p.batch.max_q, std::max(1, few.to / few.group));
+        if ((long long)p.batch.seqs * few.join_tokens > 2LL * p.batch.tokens) few.join_tokens = 0;
         few.by_join = divisor(few.join_tokens);
         r.joins = (few.join_tokens ? (long long)p.batch.seqs * few.join_tokens : p.batch.tokens) * p.heads;
-        const size_t slots = (size_t)p.batch.tokens * p.heads * few.slots, head = (slots * 2 * sizeof(float) + 15) / 16 * 16;
+        const size_t slots = (size_t)r.joins * few.slots, head = (slots * 2 * sizeof(float) + 15) / 16 * 16;
         r.workspace = head + slots * p.cache.head_dim * sizeof(float);
         few.ml = r.many.ml = p.ws;
         few.o = r.many.o = (float*)((char*)p.ws + head);
@@ -810,7 +816,7 @@ static void launch_paged(const PagedPlan& r, unsigned few, unsigned many, unsign
 int launch_paged_attention(const PagedAttention& p, hipStream_t stream) {
     const PagedPlan r = paged_plan(p);
     const long long few = paged_grid(r.few), many = paged_grid(r.many), joins = r.joins;
-    if (few > 0x7fffffffLL || many > 0x7fffffffLL || joins > 0x7fffffffLL) { set_error("attention_paged: grid too large"); return STRAIT_E_SHAPE; }
+    if (few > MOST_WORKGROUPS || many > MOST_WORKGROUPS || joins > MOST_WORKGROUPS) { set_error("attention_paged: grid too large"); return STRAIT_E_SHAPE; }
     const bool i8 = p.cache.type == STRAIT_KV_I8;
     if (p.cache.head_dim == 64) i8 ? launch_paged<64, true>(r, (unsigned)few, (unsigned)many, (unsigned)joins, stream) : launch_paged<64, false>(r, (unsigned)few, (unsigned)many, (unsigned)joins, stream);
     else i8 ? launch_paged<128, true>(r, (unsigned)few, (unsigned)many, (unsigned)joins, stream) : launch_paged<128, false>(r, (unsigned)few, (unsigned)many, (unsigned)joins, stream);

@@ -67,6 +67,7 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const half_t* __rest
 }
 
 int launch_quantize_rows(const half_t* x, int M, int K, long long pitch, int8_t* q, float* scale, int hp, hipStream_t stream) {
+    if (M > MOST_WORKGROUPS) { set_error("quantize_rows: grid too large"); return STRAIT_E_SHAPE; }
     if (K <= 64 * 8 * QUANTIZE_KEPT) hipLaunchKernelGGL((quantize_rows_kernel<64>), dim3((unsigned)((M + 3LL) / 4)), dim3(256), 0, stream, x, M, K / 8, pitch, q, scale, hp);
     else hipLaunchKernelGGL((quantize_rows_kernel<256>), dim3((unsigned)M), dim3(256), 0, stream, x, M, K / 8, pitch, q, scale, hp);
     hipError_t e = hipGetLastError();

@@ -107,6 +107,30 @@ def test_attention_paged_says_what_workspace_it_needs():
         assert attend(cache(), long, ws=A + 4) == INVALID
 
 
+def test_what_a_launch_cannot_hold_is_refused():
+    assert quantize(M=1 << 24) == SHAPE and quantize(M=1 << 24, K=4096, pitch=4096) == SHAPE
+    big = 0x7fffffff
+    for m, n in ((1, big), (20, big), (big, 1), (big, 64), (1 << 24, 1 << 24), (big, big)):
+        assert gemm(M=m, N=n, K=16) == SHAPE, (m, n)
+    for call in (append, attend):
+        assert call(cache(), batch(max_kv=(1 << 29) + 1, table_pitch=1 << 24)) == SHAPE and "max_kv" in S.last_error()
+    assert append(cache(kv_heads=4), batch(seqs=1 << 23, tokens=1 << 23, max_q=1), pk=512, pv=512) == SHAPE
+    assert attend(cache(), batch(seqs=1 << 20, tokens=1 << 20, max_q=1, max_kv=1 << 20, table_pitch=1 << 14), heads=2, ws_bytes=1 << 62) == SHAPE
+
+
+def test_a_product_goes_into_its_residual_in_fp16_only():
+    assert gemm(res=A, y=A, out_f32=1) == INVALID and "y may be res" in S.last_error()
+
+
+def test_parts_take_room_only_for_what_is_joined():
+    """A long prompt beside single tokens: room for the parts of a few tokens of each sequence, not of the prompt's."""
+    need = C.c_size_t(0)
+    b = batch(seqs=8, tokens=8192 + 7, max_q=8192, max_kv=131072, table_pitch=2048)
+    assert S.lib.strait_k_attention_paged_workspace(C.byref(cache()), C.byref(b), 8, 0, 0, C.byref(need)) == OK
+    rows = 8 * 4 * 8                                      # sequences, tokens of 16 rows, heads
+    assert 0 < need.value <= rows * 131072 // 32 // 8 * (128 + 2) * 4 + 16
+
+
 @pytest.mark.parametrize("positions,dim,base", [(1, 2, 10000.0), (70001, 64, 10000.0), (500, 128, 500000.0)])
 def test_rope_table(positions, dim, base):
     t = S.rope_table(positions, dim, base)

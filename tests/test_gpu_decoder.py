@@ -329,6 +329,17 @@ def test_kv_append_in_place_without_queries_and_without_tokens(S):
         assert all(x is None or np.array_equal(x, y) for x, y in zip(before, w.taken_back()))
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_kv_append_rotates_queries_in_place(S, interleaved):
+    for new, group, dim in (([1] * 7, 8, 128), ([900, 1200], 2, 64)):             # a workgroup and a wavefront for a token
+        w = World(S, 17, new, [i * 5 for i in range(len(new))], 2, group, dim, 64, False).on_gpu()
+        qkv, q, k, v, rope = append_inputs(w, dim)
+        held = dev(S, q)
+        got = S.k_kv_append(w.cache, w.batch, dev(S, k), dev(S, v), q=held, rope=dev(S, rope), interleaved=interleaved, q_out=held)
+        assert got is held
+        check_append(w, q, k, v, rope, interleaved, host(held), w.taken_back())
+
+
 def test_kv_append_int8_of_odd_numbers(S):
     """Infinities count as 65504 and NaN as 0; pages of zeros have scale 0; a fresh page's old scale and codes may be anything; a scale that does not grow leaves old codes alone."""
     w = World(S, 14, [4, 5, 3, 2], [0, 64, 7, 7], 2, 1, 64, 64, True)
@@ -503,6 +514,30 @@ def test_attention_paged_extreme_scores(S, i8, new, past):
         w.v[g] *= np.float16(500)
         w.k[w.table[0, 2]] *= np.float16(20)
     check_attention(S, w)
+
+
+@pytest.mark.parametrize("i8", [False, True], ids=["fp16", "int8"])
+@pytest.mark.parametrize("new,past", [([1, 1], [900, 3]), ([150, 5], [100, 0])])
+def test_attention_paged_extreme_scales(S, i8, new, past):
+    """A score scale that leaves nothing of the scores (also times the cache's), and pages whose values' or keys' scales are the smallest numbers, 0, or the largest allowed."""
+    for scale in (1e-30, 1e-38, 1e-45):
+        check_attention(S, World(S, 40, new, past, 1, 4, 64, 32, i8), scale=scale)
+        check_attention(S, World(S, 41, new, past, 1, 4, 64, 32, i8), 40, 3, scale=scale)
+    if i8:
+        for odd in (1e-45, 1e-40, 1e-30, 2.0 ** -60, 1e-15, 0.0, 4096.0):
+            w = World(S, 42, new, past, 1, 4, 64, 32, i8)
+            few = w.table[0, 1:3]
+            w.vs[few] = np.float32(odd)
+            w.v[few] //= 12 if odd > 1 else 1
+            if odd < 1:
+                w.ks[w.table[0, 2:4]] = np.float32(odd)
+            check_attention(S, w)
+
+
+@pytest.mark.parametrize("i8", [False, True], ids=["fp16", "int8"])
+@pytest.mark.parametrize("new,past", [([16] + [1] * 39, [2000] + [i * 97 % 1500 for i in range(40 - 1)]), ([700] + [1] * 12, [900] + [2000 - i for i in range(12)])], ids=["few", "both"])
+def test_attention_paged_joins_tokens_by_their_sequences_or_as_they_come(S, i8, new, past):
+    check_attention(S, World(S, 43, new, past, 8, 1, 64, 64, i8))
 
 
 def test_attention_paged_shared_pages_and_strided_queries(S):
