@@ -115,7 +115,7 @@ def test_what_a_launch_cannot_hold_is_refused():
     for call in (append, attend):
         assert call(cache(), batch(max_kv=(1 << 29) + 1, table_pitch=1 << 24)) == SHAPE and "max_kv" in S.last_error()
     assert append(cache(kv_heads=4), batch(seqs=1 << 23, tokens=1 << 23, max_q=1), pk=512, pv=512) == SHAPE
-    assert attend(cache(), batch(seqs=1 << 20, tokens=1 << 20, max_q=1, max_kv=1 << 20, table_pitch=1 << 14), heads=2, ws_bytes=1 << 62) == SHAPE
+    assert attend(cache(), batch(seqs=1 << 24, max_q=1), heads=2, ws_bytes=1 << 62) == SHAPE
 
 
 def test_a_product_goes_into_its_residual_in_fp16_only():
