@@ -160,7 +160,13 @@ __global__ void __launch_bounds__(64 * WGM * WGN, (tile_waves_per_simd<BM, BN, W
             const int m = row_of(b, i);
 #pragma unroll
             for (int j = 0; j < 8; ++j) res[i][j] = (half_t)0.f;
-            if (p.res && m < p.M && many >= 8) res[i] = ((const AnyHalf8*)(p.res + (long long)m * p.N + n))->h;
+            if (!p.res || m >= p.M || many <= 0) continue;
+            const half_t* from = p.res + (long long)m * p.N + n;
+            if (many >= 8) res[i] = ((const AnyHalf8*)from)->h;
+            else {                                     // (the last channels: seven loads under way at once, not one for each that there is in turn)
+#pragma unroll
+                for (int j = 0; j < 7; ++j) res[i][j] = from[j < many ? j : 0];
+            }
         }
     };
     if (TMB == 1) load_res(0);
@@ -287,15 +293,6 @@ __global__ void __launch_bounds__(64 * WGM * WGN, (tile_waves_per_simd<BM, BN, W
             const int m = row_of(b, i);
             if (m >= p.M || many <= 0) continue;
             const long long at = (long long)m * p.N + n;
-            if (many < 8) {                            // the last channels
-#pragma unroll 1
-                for (int j = 0; j < many; ++j) {
-                    const float y = finish(from[j], xs[i], channels[c0 + j], channels[BN + c0 + j], p.res ? (float)p.res[at + j] : 0.f, ACT);
-                    if (p.out_f32) ((float*)p.y)[at + j] = y;
-                    else ((half_t*)p.y)[at + j] = (half_t)y;
-                }
-                continue;
-            }
             floatx4 y[2];
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
@@ -303,7 +300,14 @@ __global__ void __launch_bounds__(64 * WGM * WGN, (tile_waves_per_simd<BM, BN, W
 #pragma unroll
                 for (int j = 0; j < 4; ++j) y[k][j] = finish((k ? hi : lo)[j], xs[i], ws[j], bias[j], (float)res[i][4 * k + j], ACT);
             }
-            if (p.out_f32) {
+            if (many < 8) {
+#pragma unroll
+                for (int j = 0; j < 7; ++j) {
+                    if (j >= many) continue;
+                    if (p.out_f32) ((float*)p.y)[at + j] = y[j >> 2][j & 3];
+                    else ((half_t*)p.y)[at + j] = (half_t)y[j >> 2][j & 3];
+                }
+            } else if (p.out_f32) {
                 *(AnyFloat4*)((float*)p.y + at) = AnyFloat4{y[0]};
                 *(AnyFloat4*)((float*)p.y + at + 4) = AnyFloat4{y[1]};
             } else {
