@@ -6,10 +6,11 @@
 //
 //   gemm_i8_stream_kernel, few rows: bound by the weights' bytes.  A workgroup of 8 wavefronts has 16 NT channels and shares the reduction
 //   out in pieces of 256; weights go from memory to registers in the layout of v_mfma_i32_16x16x64_i8's operand, a piece ahead, and each byte is read
-//   once on the whole chip.  The partial sums meet in LDS as integers.
+//   once on the whole chip.  The partial sums meet in LDS as integers.  1 x 4096 x 4096 6.2 us (2.7 TB/s), 16 x 16384 x 4096 13.0 us (5.2 TB/s).
 //
 //   gemm_i8_tile_kernel: bound by the matrix pipes.  Slices of 128 of the reduction travel to a ring in LDS without passing through registers, the operands of
-//   the next MFMAs are read while the current ones run, and one barrier per slice hands a stage on.
+//   the next MFMAs are read while the current ones run, and one barrier per slice hands a stage on.  8192 x 16384 x 4096 520 to 530 us, 2.1 POP/s, where the library's largest products
+//   reach 2.15 and MFMAs on registers alone 2.3: the card's power.  An epilogue for each activation: one that asks at every output took 15 to 20 % of the whole kernel's time.
 #include <type_traits>
 
 #include "activation.hpp"

@@ -2,19 +2,31 @@
 //
 //   out[t, h] = sum_j softmax_j( scale q[t, h] . k_j ) v_j  over the keys j <= p  with  window == 0  or  p - j < window  or  j < sinks
 //
-// The rows of a tile are (token, head of the group) pairs of one kv head: all of them read the same keys.  The keys that any of them sees, in blocks of
-// 32 that lie on one page each, are shared out over workgroups (parts of `per_part` blocks, whose results a second launch joins) and over a workgroup's four
-// wavefronts, which take every fourth block:
+// The rows of a tile are (token, head of the group) pairs of one kv head: all of them read the same keys.  The keys that any of them sees come in blocks of
+// 32 that lie on one page each.  One pass with a running maximum, which follows the true one only where that is more than 8 (in log2) ahead: probabilities stay below 2^8, and
+// the output is rescaled a few times in all.  Scores, statistics and outputs are fp32; the probabilities are rounded to fp16, half a step each, to be an operand of the second product.
+//
+//   paged_stream_kernel, 16 or 32 rows (steps of single tokens): bound by the cache's bytes.  Blocks are shared out over workgroups (parts of `per_part` blocks, whose
+//   results a second launch joins) and over a workgroup's four wavefronts, which take every fourth block and meet only at the end:
 //   - a wavefront's page numbers and scales are fetched at once, a lane for each block, and named by v_readlane; the next block's bytes are on their way to
-//     registers while a block is worked on;
+//     registers while a block is worked on, and none goes through LDS;
 //   - scores^T = K Q^T with v_mfma_f32_16x16x32_f16: a lane names 16 bytes of a key, as they lie in memory, and Q is enumerated in the same order; it then holds
 //     8 of the block's keys for ONE row;
 //   - an int8 code becomes fp16 by way of the number 2^-24 (code + 128), a subnormal whose bits are the code's: one fused multiply-add makes
 //     code 2^-9 of it, exactly.  The scale of the block's page multiplies the scores and the block's share of the output, in fp32;
-//   - the probabilities, rounded to fp16, are the "B" operand of out^T = V^T P^T as they are, keys enumerated in the order that the scores came in; V^T's lanes
-//     read 8 keys at D / 16 dimensions each and exchange bytes within a lane;
-//   - one pass with a running maximum, which follows the true one only where that is more than 8 (in log2) ahead: probabilities stay below 2^8, and the
-//     output is rescaled a few times in all.
+//   - the probabilities are the "B" operand of out^T = V^T P^T as they are, keys enumerated in the order that the scores came in; V^T's lanes
+//     read 8 keys at D / 16 dimensions each and exchange bytes within a lane.
+//   32 sequences of 1000 to 16383 tokens, 8 heads of 128 for 32, int8: 123 us, 4.6 TB/s with the join; 24 of 60000 and more, 4 heads for 32, fp16, the last 4096 and 4 of them seen: 48 us, 4.2 TB/s.
+//   One sequence of 4100: 10.5 us, the latency of two launches.
+//
+//   paged_tile_kernel, 128 rows (prompts and their chunks): bound by the wavefronts' own chain of products, powers and products (at two wavefronts to a SIMD, which the output's registers
+//   allow, neither pipe is full; leaving out any one of the products, the powers or the operands' reads saves little, the staging a fifth).
+//   - 64 keys at a time go through LDS, which holds them twice as fp16: a block is on its way to registers while the one before it is worked on, and becomes fp16 on its way to LDS, once
+//     for all four wavefronts;
+//   - scores^T with v_mfma_f32_32x32x16_f16, a row to a lane and its partner 32 lanes on; V^T's operands come from LDS transposed (ds_read_b64_tr_b16);
+//   - an int8 value's power of two is its page's, exact in fp16, and the rest of the page's scale goes into the probabilities (see look_up).
+//   Four chunks of 1200 to 2048 tokens behind up to 2048, 8 heads of 128 for 32, int8: 254 us, 720 TFLOP/s of what the masks leave; five of 333 to 4001 with a window of 1024, 12 heads
+//   of 64, fp16: 68 us, 445 TFLOP/s.
 #include <algorithm>
 #include <type_traits>
 
