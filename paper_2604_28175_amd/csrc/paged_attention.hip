@@ -19,14 +19,16 @@
 //   32 sequences of 1000 to 16383 tokens, 8 heads of 128 for 32, int8: 123 us, 4.6 TB/s with the join; 24 of 60000 and more, 4 heads for 32, fp16, the last 4096 and 4 of them seen: 48 us, 4.2 TB/s.
 //   One sequence of 4100: 10.5 us, the latency of two launches.
 //
-//   paged_tile_kernel, 128 rows (prompts and their chunks): bound by the wavefronts' own chain of products, powers and products (at two wavefronts to a SIMD, which the output's registers
-//   allow, neither pipe is full; leaving out any one of the products, the powers or the operands' reads saves little, the staging a fifth).
-//   - 64 keys at a time go through LDS, which holds them twice as fp16: a block is on its way to registers while the one before it is worked on, and becomes fp16 on its way to LDS, once
-//     for all four wavefronts;
+//   paged_tile_kernel, 128 rows (prompts and their chunks): bound by the wavefronts' own chain of reads, products, powers and products (at two wavefronts to a SIMD, which the output's registers
+//   allow at 128 dimensions, no unit is full: vector instructions 60 % of the time, LDS 50, the matrix pipes 42).
+//   - 64 keys at a time go through LDS, which holds them twice as fp16: two blocks are worked on, the next two become fp16 on their way from registers to LDS, once
+//     for all four wavefronts, and the two after them are on their way from memory;
+//   - a wavefront issues in order, so its products and its vector instructions are woven by hand: the way to LDS between the products of the scores, a step's powers between
+//     the products that the step before it goes into (254 -> 243 us and 68 -> 63 us in the calls below; blocks that none of a wavefront's rows see are worked on all the same, which costs nothing: the others are waited for);
 //   - scores^T with v_mfma_f32_32x32x16_f16, a row to a lane and its partner 32 lanes on; V^T's operands come from LDS transposed (ds_read_b64_tr_b16);
 //   - an int8 value's power of two is its page's, exact in fp16, and the rest of the page's scale goes into the probabilities (see look_up).
-//   Four chunks of 1200 to 2048 tokens behind up to 2048, 8 heads of 128 for 32, int8: 254 us, 720 TFLOP/s of what the masks leave; five of 333 to 4001 with a window of 1024, 12 heads
-//   of 64, fp16: 68 us, 445 TFLOP/s.
+//   Four chunks of 1200 to 2048 tokens behind up to 2048, 8 heads of 128 for 32, int8: 243 us, 755 TFLOP/s of what the masks leave; five of 333 to 4001 with a window of 1024, 12 heads
+//   of 64, fp16: 63 us, 482 TFLOP/s.
 #include <algorithm>
 #include <type_traits>
 
@@ -473,12 +475,12 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
     auto kswz = [](int row) { return D == 128 ? row & 15 : row & 7; };
     auto vswz = [](int row) { return D == 128 ? (row & 3) << 2 | (row & 1) : (row & 2) << 1; };
     uintx4 raw[NI];
-    // A lane of each wavefront holds what is to be known of a block: where it begins (behind all rows: not seen) and lies in the cache, and its scales; two masks say
-    // which of the 64 blocks all of the wavefront's rows see whole, and which none of them sees.
+    // A lane of each wavefront holds what is to be known of a block: where it begins (behind all rows: not seen) and lies in the cache, and its scales; masks say
+    // which of the 64 blocks all of the wavefront's rows see whole, and of which each key is seen by some row of the tile.
     int k0s = 0;
     unsigned from_lo = 0, from_hi = 0;
     float kcs = c, vpow = 1.f, vlog = 0.f, vinv = 1.f;
-    unsigned long long full = 0, none = 0;
+    unsigned long long full = 0, open = 0;
     auto look_up = [&](int first) __attribute__((always_inline)) {
         k0s = NOWHERE;
         from_lo = from_hi = 0;
@@ -503,8 +505,8 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
                 }
             }
         }
-        none = __ballot(!any || k0s > hi || (p.window && lo - (k0s + KEYS - 1) >= p.window && k0s >= p.sinks));
         full = __ballot(k0s + KEYS - 1 <= lo && (!p.window || hi - k0s < p.window || k0s + KEYS - 1 < p.sinks));
+        if (!I8) open = __ballot(k0s + KEYS - 1 <= t.hi && (!p.window || t.lo - k0s < p.window || k0s + KEYS - 1 < p.sinks));
     };
     auto of_block = [](int v, int n) __attribute__((always_inline)) { return __builtin_amdgcn_readlane(v, n); };
     auto of_blockf = [](float v, int n) __attribute__((always_inline)) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), n)); };
@@ -515,32 +517,40 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
             const int blk = n + (PER_ROW * KEYS >= NT ? x * NT % HALF / (PER_ROW * KEYS) : __builtin_amdgcn_readfirstlane(row >> 5));
             const unsigned long long from = (unsigned long long)(unsigned)of_block((int)from_hi, blk) << 32 | (unsigned)of_block((int)from_lo, blk);
             raw[x] = *(const uintx4*)((const char*)(v ? p.cache.v : p.cache.k) + from + (unsigned)(rem & (KEYS * PER_ROW - 1)) * 16u);
-            if constexpr (!I8) {                       // what no row of the tile sees may be anything: it becomes zeros (of int8 it is finite, and its probability 0)
-                const int key = of_block(k0s, blk) + (row & 31);
-                if (!(key <= t.hi && (!p.window || t.lo - key < p.window || key < p.sinks))) raw[x] = uintx4{0, 0, 0, 0};
-            }
         }
     };
-    auto stage = [&](int n, int st) __attribute__((always_inline)) {
+    // Of what was fetched of blocks n and n + 1, the q-th of 2 D / 16 equal shares: a word of codes, or half a piece (that is, every second time a piece).
+    constexpr int SHARES = D / 8;
+    static_assert(I8 ? SHARES == 4 * NI : SHARES == 2 * NI, "shares");
+    half8 widened;
+    auto stage = [&](int q, int n, int st) __attribute__((always_inline)) {
+        if (!I8 && q % 2 == 0) return;
+        const int x = I8 ? q / 4 : q / 2, v = x * NT >= HALF, rem = x * NT + tid - v * HALF, row = rem / PER_ROW, piece = rem % PER_ROW;
+        char* dst = tile_lds + st * STAGE + v * (TILE_KEYS * ROW) + row * ROW;
+        const int swz = v ? vswz(row) : kswz(row);
+        if constexpr (I8) {
+            unsigned w = raw[x][q % 4];
+            asm volatile("" : "+v"(w));                 // (its bytes are spread here, not ahead of all products)
+            w ^= 0x80808080u;
+            const half_t by = v ? (half_t)of_blockf(vpow, __builtin_amdgcn_readfirstlane(n + (row >> 5))) : (half_t)1.f;
 #pragma unroll
-        for (int x = 0; x < NI; ++x) {
-            const int v = x * NT >= HALF, rem = x * NT + tid - v * HALF, row = rem / PER_ROW, piece = rem % PER_ROW;
-            char* dst = tile_lds + st * STAGE + v * (TILE_KEYS * ROW) + row * ROW;
-            const int swz = v ? vswz(row) : kswz(row);
-            if constexpr (I8) {
-                const uintx4 w = raw[x] ^ 0x80808080u;
-                const half_t by = v ? (half_t)of_blockf(vpow, __builtin_amdgcn_readfirstlane(n + (row >> 5))) : (half_t)1.f;
-                half8 y[2];
-#pragma unroll
-                for (int e = 0; e < 16; e += 2) {
-                    const half2_t z = scaled_codes(w[e >> 2], e & 2, by);
-                    y[e >> 3][e & 7] = z[0];
-                    y[e >> 3][(e & 7) + 1] = z[1];
-                }
-                *(half8*)(dst + ((2 * piece) ^ swz) * 16) = y[0];
-                *(half8*)(dst + ((2 * piece + 1) ^ swz) * 16) = y[1];
-            } else *(uintx4*)(dst + (piece ^ swz) * 16) = raw[x];
+            for (int e = 0; e < 4; e += 2) {
+                const half2_t z = scaled_codes(w, e, by);
+                widened[q % 2 * 4 + e] = z[0];
+                widened[q % 2 * 4 + e + 1] = z[1];
+            }
+            if (q % 2) *(half8*)(dst + ((2 * piece + q % 4 / 2) ^ swz) * 16) = widened;
+        } else {
+            if ((open >> (n & 63) & 3) != 3) {                // what no row of the tile sees may be anything: it becomes zeros (of int8 it is finite, and its probability 0)
+                const int key = of_block(k0s, __builtin_amdgcn_readfirstlane(n + (row >> 5))) + (row & 31);
+                if (!(key <= t.hi && (!p.window || t.lo - key < p.window || key < p.sinks))) raw[x] = uintx4{0, 0, 0, 0};
+            }
+            *(uintx4*)(dst + (piece ^ swz) * 16) = raw[x];
         }
+    };
+    auto stage_all = [&](int n, int st) __attribute__((always_inline)) {
+#pragma unroll
+        for (int q = 0; q < SHARES; ++q) stage(q, n, st);
     };
 
     // V: lane i of a group of 16 names keys 4 lh + (i >> 2), dimensions 16 ((lane >> 4) & 1) + 4 (i & 3) .. + 3 of a 16-key step and 32 dimensions, and receives
@@ -556,20 +566,19 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
     // whether a row sees the key `off` behind some key of which it is `past` tokens past and which is `sinks` keys in front of the last sink
     const int window = p.window ? p.window : NO_WINDOW;
     auto sees = [&](int off, int past, int sinks) __attribute__((always_inline)) { return off <= past && (off > past - window || off < sinks); };
-    auto work = [&](int n, int st, bool mask) __attribute__((always_inline)) {
+    // Blocks n and n + 1 from stage st.  A wavefront issues in order, and a product holds the matrix pipe for 8 vector instructions: so that these run beside it, each product of the scores
+    // is followed by a share of the next two blocks' way to LDS, and each of the output by powers that the next ones need.
+    auto work = [&](int n, int st, bool mask, auto scores_done) __attribute__((always_inline)) {
         const char* ks0 = tile_lds + st * STAGE;
         floatx16 sc[2];                                // lane holds its row against keys 32 kb + 8 g + 4 lh + j of the tile (v = 4 g + j)
         float kc[2], top = -INFINITY;
         half8 kf[D / 16];
         auto read_key = [&](int kb, int ks) __attribute__((always_inline)) { kf[ks] = *(const half8*)(ks0 + (kb * 32 + l32) * ROW + (((ks * 2 + lh) ^ kswz(l32)) << 4)); };
-        // (the barriers keep the scheduler from holding more operands than there are registers for)
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks) read_key(0, ks);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
-            kc[kb] = I8 ? of_blockf(kcs, n + kb) : c;
-            const int k0 = of_block(k0s, n + kb);
 #pragma unroll
             for (int v = 0; v < 16; ++v) sc[kb][v] = 0.f;
 #pragma unroll
@@ -577,10 +586,19 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
                 sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[ks], qf[ks], sc[kb], 0, 0, 0);
                 __builtin_amdgcn_sched_barrier(0);
                 if (kb == 0) read_key(1, ks);
+                stage(kb * (D / 16) + ks, n + 2, st ^ 1);      // (behind the last block: what is there already, where nobody looks)
+                __builtin_amdgcn_sched_barrier(0);
             }
-            __builtin_amdgcn_sched_barrier(0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        scores_done();
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            kc[kb] = I8 ? of_blockf(kcs, n + kb) : c;
             if (mask) {
                 asm volatile("");                      // (a branch: most blocks have nothing to mask)
+                const int k0 = of_block(k0s, n + kb);
 #pragma unroll
                 for (int v = 0; v < 16; ++v) sc[kb][v] = sees(8 * (v >> 2) + (v & 3), pos - k0 - 4 * lh, p.sinks - k0 - 4 * lh) ? sc[kb][v] : -INFINITY;
             }
@@ -599,62 +617,77 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
 #pragma unroll
                 for (int v = 0; v < 16; ++v) o[db][v] *= alpha;
         }
+        __builtin_amdgcn_sched_barrier(0);
         const float ref = m > -INFINITY ? m : 0.f;
+        // four steps of 16 keys each
+        half8 pf[2], vf[D / 32];
+        float off[2], sum[2] = {0.f, 0.f};
+        unsigned vbase[D / 32];
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            const float off = (I8 ? of_blockf(vlog, n + kb) : 0.f) - ref;
-            float sum = 0.f;
+        for (int kb = 0; kb < 2; ++kb) off[kb] = (I8 ? of_blockf(vlog, n + kb) : 0.f) - ref;
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                half8 pf, vf[D / 32];
+        for (int db = 0; db < D / 32; ++db) {
+            vbase[db] = vaddr[db] + (unsigned)(st * STAGE);
+            asm("" : "+v"(vbase[db]));                 // (one addition, and what follows in the instructions' offsets)
+        }
+        auto read_values = [&](int step, int db) __attribute__((always_inline)) {
+            const fp16x4 lo4 = vread(vbase[db] + step * 16 * ROW), hi4 = vread(vbase[db] + (step * 16 + 8) * ROW);
 #pragma unroll
-                for (int db = 0; db < D / 32; ++db) {
-                    const unsigned at = vaddr[db] + (unsigned)(st * STAGE + (kb * 32 + half * 16) * ROW);
-                    const fp16x4 lo4 = vread(at), hi4 = vread(at + 8 * ROW);
+            for (int j = 0; j < 4; ++j) { vf[db][j] = (half_t)lo4[j]; vf[db][4 + j] = (half_t)hi4[j]; }
+        };
+        // two of a step's 8 probabilities of this lane: computed and summed here, neither ahead of the products nor behind them all
+        auto powers = [&](int step, int j) __attribute__((always_inline)) {
+            const int kb = step >> 1, at = 8 * (step & 1) + j;
+            float x = sc[kb][at], y = sc[kb][at + 1];
+            asm volatile("" : "+v"(x), "+v"(y));
+            x = __builtin_amdgcn_exp2f(__builtin_fmaf(x, kc[kb], off[kb]));
+            y = __builtin_amdgcn_exp2f(__builtin_fmaf(y, kc[kb], off[kb]));
+            sum[kb] += x + y;
+            asm volatile("" : "+v"(sum[kb]));
+            pf[step & 1][j] = (half_t)x;
+            pf[step & 1][j + 1] = (half_t)y;
+        };
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) { vf[db][j] = (half_t)lo4[j]; vf[db][4 + j] = (half_t)hi4[j]; }
-                }
+        for (int db = 0; db < D / 32; ++db) read_values(0, db);
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) powers(0, j);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int step = 0; step < 4; ++step)
+#pragma unroll
+            for (int db = 0; db < D / 32; ++db) {
+                o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[db], pf[step & 1], o[db], 0, 0, 0);
                 __builtin_amdgcn_sched_barrier(0);
+                if (step < 3) {
+                    constexpr int EACH = 8 / (D / 32);
+                    read_values(step + 1, db);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float pv = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[kb][8 * half + j], kc[kb], off));
-                    sum += pv;
-                    pf[j] = (half_t)pv;
+                    for (int j = 0; j < EACH; j += 2) powers(step + 1, db * EACH + j);
                 }
-#pragma unroll
-                for (int db = 0; db < D / 32; ++db) o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[db], pf, o[db], 0, 0, 0);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            l = I8 ? __builtin_fmaf(sum, of_blockf(vinv, n + kb), l) : l + sum;
-        }
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) l = I8 ? __builtin_fmaf(sum[kb], of_blockf(vinv, n + kb), l) : l + sum[kb];
     };
 
-    if (begin < end) {
-        look_up(begin);
+    // 64 blocks that are looked up at once: two of them in LDS and worked on, two in registers on their way there, two more requested once these are written
+    for (int first = begin; first < end; first += 64) {
+        const int count = end - first < 64 ? end - first : 64;
+        look_up(first);
         fetch(0);
-        stage(0, 0);
+        stage_all(0, 0);
+        if (count > 2) fetch(2);
         __syncthreads();
-        int st = 0, n = 0;                             // tile of blocks n, n + 1 of those that were looked up
-        for (int first = begin; first < end;) {
-            const bool skip = (none >> n & 3) == 3, whole = (full >> n & 3) == 3;
-            const int nn = n + 2;
-            const bool more = first + 2 < end;
-            // (a look-up replaces what the current tile still needs: it waits for the tile's end)
-            const bool ahead = more && nn < 64;
-            if (ahead) fetch(nn);
-            if (!skip) work(n, st, !whole);
-            n = nn;
-            first += 2;
-            if (more) {
-                if (!ahead) {
-                    look_up(first);
-                    n = 0;
-                    fetch(0);
+        for (int n = 0, st = 0; n < count; n += 2, st ^= 1) {
+            auto next = [&]() __attribute__((always_inline)) {
+                if (n + 4 < count) fetch(n + 4);
+                else {
+#pragma unroll
+                    for (int x = 0; x < NI; ++x) raw[x] = uintx4{0, 0, 0, 0};      // (rather than keep what is there, in other registers than what a fetch brings)
                 }
-                stage(n, st ^ 1);
-            }
+            };
+            work(n, st, (full >> n & 3) != 3, next);
             __syncthreads();
-            st ^= 1;
         }
     }
     const float2 ll = halves_of(l);
