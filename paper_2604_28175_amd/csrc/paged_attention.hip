@@ -470,10 +470,12 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
     float m = -INFINITY, l = 0.f;
     const float c = fmaxf(p.scale * 1.44269504088896340736f, 0x1p-126f);
 
-    // ---- memory -> registers -> LDS.  Chunk q of 16 bytes of row r lies at q ^ (r % 16) for K (D = 64: r % 8), whose operand is 16 rows at one chunk.  V's
-    // operand is 4 rows at 4 chunks at a time: the rows' bits go to the chunk's bits above those (and to the lowest, for the sake of the stores)
-    auto kswz = [](int row) { return D == 128 ? row & 15 : row & 7; };
-    auto vswz = [](int row) { return D == 128 ? (row & 3) << 2 | (row & 1) : (row & 2) << 1; };
+    // ---- memory -> registers -> LDS.  Chunk q of 16 bytes of row r lies at q ^ (r % 16) for K (D = 64: r / 2 % 8, two rows to the width of the banks), whose operand is 16 rows at one
+    // chunk.  V's operand is 4 rows at 4 chunks at a time: the rows' bits go to the chunk's bits above those.  Eight lanes store at a time, and codes go to every second chunk: so that they meet
+    // no bank twice, they are those of two rows (lanes' bits 2 and 3 change places) whose chunks differ in the lowest bit.
+    auto kswz = [](int row) { return D == 128 ? row & 15 : row >> 1 & 7; };
+    auto vswz = [](int row) { return D == 128 ? (row & 3) << 2 | (row & 1) : (row & 2) << 1 | (row >> 1 & 1); };
+    const int ptid = I8 ? (tid & ~12) | (tid & 4) << 1 | (tid & 8) >> 1 : tid;
     uintx4 raw[NI];
     // A lane of each wavefront holds what is to be known of a block: where it begins (behind all rows: not seen) and lies in the cache, and its scales; masks say
     // which of the 64 blocks all of the wavefront's rows see whole, and of which each key is seen by some row of the tile.
@@ -513,7 +515,7 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
     auto fetch = [&](int n) __attribute__((always_inline)) {       // blocks n and n + 1 of the 64 that were looked up
 #pragma unroll
         for (int x = 0; x < NI; ++x) {
-            const int v = x * NT >= HALF, rem = x * NT + tid - v * HALF, row = rem / PER_ROW;
+            const int v = x * NT >= HALF, rem = x * NT + ptid - v * HALF, row = rem / PER_ROW;
             const int blk = n + (PER_ROW * KEYS >= NT ? x * NT % HALF / (PER_ROW * KEYS) : __builtin_amdgcn_readfirstlane(row >> 5));
             const unsigned long long from = (unsigned long long)(unsigned)of_block((int)from_hi, blk) << 32 | (unsigned)of_block((int)from_lo, blk);
             raw[x] = *(const uintx4*)((const char*)(v ? p.cache.v : p.cache.k) + from + (unsigned)(rem & (KEYS * PER_ROW - 1)) * 16u);
@@ -525,7 +527,7 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
     half8 widened;
     auto stage = [&](int q, int n, int st) __attribute__((always_inline)) {
         if (!I8 && q % 2 == 0) return;
-        const int x = I8 ? q / 4 : q / 2, v = x * NT >= HALF, rem = x * NT + tid - v * HALF, row = rem / PER_ROW, piece = rem % PER_ROW;
+        const int x = I8 ? q / 4 : q / 2, v = x * NT >= HALF, rem = x * NT + ptid - v * HALF, row = rem / PER_ROW, piece = rem % PER_ROW;
         char* dst = tile_lds + st * STAGE + v * (TILE_KEYS * ROW) + row * ROW;
         const int swz = v ? vswz(row) : kswz(row);
         if constexpr (I8) {
