@@ -543,7 +543,7 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
             }
             if (q % 2) *(half8*)(dst + ((2 * piece + q % 4 / 2) ^ swz) * 16) = widened;
         } else {
-            if ((open >> (n & 63) & 3) != 3) {                // what no row of the tile sees may be anything: it becomes zeros (of int8 it is finite, and its probability 0)
+            if ((open >> n & 3) != 3) {                // what no row of the tile sees may be anything: it becomes zeros (of int8 it is finite, and its probability 0)
                 const int key = of_block(k0s, __builtin_amdgcn_readfirstlane(n + (row >> 5))) + (row & 31);
                 if (!(key <= t.hi && (!p.window || t.lo - key < p.window || key < p.sinks))) raw[x] = uintx4{0, 0, 0, 0};
             }
@@ -588,7 +588,7 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
                 sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[ks], qf[ks], sc[kb], 0, 0, 0);
                 __builtin_amdgcn_sched_barrier(0);
                 if (kb == 0) read_key(1, ks);
-                stage(kb * (D / 16) + ks, n + 2, st ^ 1);      // (behind the last block: what is there already, where nobody looks)
+                stage(kb * (D / 16) + ks, (n + 2) & 63, st ^ 1);      // (behind the last block: what is there already, where nobody looks)
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
@@ -791,7 +791,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const PagedArgs few, co
 }
 
 // How a call is launched.  Sequences with up to 16 or 32 rows of a kv head: the stream kernel, tiles of 16 or 32 rows.  More: the tile kernel, 128 rows, of which a compute unit holds
-// two.  (256 rows by eight wavefronts fill LDS half as often, but all of them stand at one barrier: chunks of four prompts 274 and 274 us, with a window 74 and 97.)  A step of
+// two, or three of 64 dimensions.  (256 rows by eight wavefronts fill LDS half as often, but all of them stand at one barrier: chunks of four prompts as fast, with a window a third slower.)  A step of
 // both kinds gets both launches.  Parts of as many blocks as give each compute unit several workgroups (tile kernel: where it would not have one).
 struct PagedPlan { PagedArgs few, many; size_t workspace; long long joins; };
 
