@@ -722,14 +722,22 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
     }
 }
 
-// Joins the parts of rows that were shared out: a workgroup per (token, head), whose threads take 4 dimensions each and every few parts.
+// Joins the parts of rows that were shared out: a workgroup per (token, head), whose threads take 4 dimensions each and every few parts.  Latency bounds it: what the first parts' places
+// hold is requested beside the sequence's lengths, which say how many parts there are.
 template <int D>
 __global__ void __launch_bounds__(256) paged_join_kernel(const PagedArgs few, const PagedArgs many) {
-    constexpr int GROUP = D / 4, GROUPS = 256 / GROUP;
+    constexpr int GROUP = D / 4, GROUPS = 256 / GROUP, AT_ONCE = 4;
     __shared__ floatx4 sums[GROUPS][GROUP];
     const PagedAttention& p = few.p;
     if (p.hp) __builtin_amdgcn_s_setprio(3);
-    const int lane = threadIdx.x & 63;
+    const int lane = threadIdx.x & 63, group = (int)threadIdx.x / GROUP, d = (int)threadIdx.x % GROUP, slots = few.slots;
+    const long long row = blockIdx.x;                  // (joined_token's number times the heads, and the head)
+    const float2* ml = (const float2*)few.ml + row * slots;
+    const floatx4* o = (const floatx4*)(few.o + row * slots * D) + d;
+    float2 mine = ml[lane < slots ? lane : 0];
+    floatx4 part[AT_ONCE];
+#pragma unroll
+    for (int k = 0; k < AT_ONCE; ++k) part[k] = o[(long long)(group + k * GROUPS < slots ? group + k * GROUPS : 0) * GROUP];
     const int bi = divide((int)blockIdx.x, few.by_q_heads), hq = (int)blockIdx.x - bi * p.heads;
     int b, i;
     if (few.join_tokens) {                             // of each sequence the first few tokens
@@ -744,6 +752,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const PagedArgs few, co
         if (i < 0) return;
     }
     const Sequence s = sequence(p.batch, b);
+    asm volatile("" : "+v"(mine.x), "+v"(mine.y), "+v"(part[0]), "+v"(part[1]), "+v"(part[2]), "+v"(part[3]));      // (requested above, whatever follows)
     if (i >= s.n) return;
     const PagedArgs& a = s.n * few.group <= few.to ? few : many;
     const int g = hq - divide(hq, a.by_group) * a.group;
@@ -751,31 +760,35 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const PagedArgs few, co
     const Blocks blocks = visible_blocks(t.lo, t.hi, p.window, p.sinks);
     const int parts = (blocks.count + a.per_part - 1) / a.per_part;
     if (parts <= 1) return;
-    const long long row = joined_token(a, b, s, i) * p.heads + hq;
-    const float2* ml = (const float2*)a.ml + row * a.slots;
-    const int group = (int)threadIdx.x / GROUP, d = (int)threadIdx.x % GROUP;
-    const floatx4* o = (const floatx4*)(a.o + row * a.slots * D) + d;
+    if (lane >= parts) mine = make_float2(-INFINITY, 0.f);
     // (every wavefront finds the maximum and the sum for itself)
-    float top = -INFINITY, sum = 0.f;
-    for (int x = lane; x < parts; x += 64) top = fmaxf(top, ml[x].x);
+    float top = mine.x, sum;
+    for (int x = lane + 64; x < parts; x += 64) top = fmaxf(top, ml[x].x);
 #pragma unroll
     for (int k = 32; k; k >>= 1) top = fmaxf(top, __shfl_xor(top, k));
     auto weight = [&](float2 v) { return v.y == 0.f ? 0.f : v.y * __builtin_amdgcn_exp2f(v.x - top); };    // (NaN stays NaN)
-    for (int x = lane; x < parts; x += 64) sum += weight(ml[x]);
+    const float my_weight = weight(mine);
+    sum = my_weight;
+    for (int x = lane + 64; x < parts; x += 64) sum += weight(ml[x]);
 #pragma unroll
     for (int k = 32; k; k >>= 1) sum += __shfl_xor(sum, k);
     floatx4 y = {0.f, 0.f, 0.f, 0.f};
-    for (int x = group; x < parts; x += 4 * GROUPS) {
-        floatx4 part[4];
-        float w[4];
+    static_assert(AT_ONCE * GROUPS <= 64, "a lane for each of the first parts");
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < AT_ONCE; ++k) {
+        const float w = __shfl(my_weight, group + k * GROUPS);
+        if (group + k * GROUPS < parts) y += part[k] * w;
+    }
+    for (int x = group + AT_ONCE * GROUPS; x < parts; x += AT_ONCE * GROUPS) {
+        float w[AT_ONCE];
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
             const int at = x + k * GROUPS;
             part[k] = o[(long long)(at < parts ? at : x) * GROUP];
             w[k] = at < parts ? weight(ml[at]) : 0.f;
         }
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
+        for (int k = 0; k < AT_ONCE; ++k)
             if (x + k * GROUPS < parts) y += part[k] * w[k];
     }
     sums[group][d] = y;
