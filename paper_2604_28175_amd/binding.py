@@ -713,6 +713,7 @@ class KvCache:
         self.width = self.kv_heads * self.head_dim
         self.desc = KvCacheDesc(_dev(k), _dev(v), _dev(k_scale), _dev(v_scale), KV_I8 if i8 else KV_F16, self.pages, self.page_tokens, self.kv_heads, self.head_dim)
         self.ref = C.byref(self.desc)
+        self.layout = (i8, *k.shape)
 
 
 class KvBatch:
@@ -728,7 +729,7 @@ class KvBatch:
             _refuse(f"page_table has {page_table.shape[0]} rows for {kv_len.shape[0]} sequences")
         self.q_start, self.kv_len, self.page_table = q_start, kv_len, page_table
         self.desc = KvBatchDesc(_dev(q_start), _dev(kv_len), _dev(page_table), kv_len.shape[0], 0, max_q, max_kv, page_table.shape[1])
-        self._of = {}
+        self._of, self._rooms = {}, {}
 
     def ref(self, tokens: int):
         """strait_kv_batch of a step of so many tokens."""
@@ -739,6 +740,18 @@ class KvBatch:
             d = KvBatchDesc.from_buffer_copy(self.desc)
             d.tokens = tokens
             r = self._of[tokens] = C.byref(d)
+        return r
+
+    def room(self, cache: KvCache, tokens: int, heads: int, window: int, sinks: int) -> int:
+        """strait_k_attention_paged_workspace of a step, which depends on sizes only."""
+        key = (tokens, heads, window, sinks, cache.layout)
+        r = self._rooms.get(key)
+        if r is None:
+            need = _sz()
+            _check(lib.strait_k_attention_paged_workspace(cache.ref, self.ref(tokens), heads, window, sinks, C.byref(need)))
+            if len(self._rooms) > 256:
+                self._rooms.clear()
+            r = self._rooms[key] = need.value
         return r
 
 
@@ -792,11 +805,10 @@ def k_attention_paged(q, cache: KvCache, batch: KvBatch, scale: float, window: i
         out = _made(stream, q.new_empty((tokens, width)))
     else:
         _dense(out, _FP16, (tokens, width), device, "out")
-    need, ref, ws = _sz(), batch.ref(tokens), None
-    _check(lib.strait_k_attention_paged_workspace(cache.ref, ref, heads, window, sinks, C.byref(need)))
-    if need.value:
-        ws = _made(stream, q.new_empty((need.value // 2,)))            # (of halfs; a multiple of 16 bytes)
-    _check(lib.strait_k_attention_paged(handle, cache.ref, ref, q.data_ptr(), pitch, heads, scale, window, sinks, out.data_ptr(), _dev(ws), need.value, hp))
+    need, ws = batch.room(cache, tokens, heads, window, sinks), None
+    if need:
+        ws = _made(stream, q.new_empty((need // 2,)))                  # (of halfs; a multiple of 16 bytes)
+    _check(lib.strait_k_attention_paged(handle, cache.ref, batch.ref(tokens), q.data_ptr(), pitch, heads, scale, window, sinks, out.data_ptr(), _dev(ws), need, hp))
     return out
 
 

@@ -17,7 +17,7 @@
 //   - the probabilities are the "B" operand of out^T = V^T P^T as they are, keys enumerated in the order that the scores came in; V^T's lanes
 //     read 8 keys at D / 16 dimensions each and exchange bytes within a lane.
 //   32 sequences of 1000 to 16383 tokens, 8 heads of 128 for 32, int8: 123 us, 4.6 TB/s with the join; 24 of 60000 and more, 4 heads for 32, fp16, the last 4096 and 4 of them seen: 48 us, 4.2 TB/s.
-//   One sequence of 4100: 10.5 us, the latency of two launches.
+//   One sequence of 4100: 9.7 us, the latency of two launches.
 //
 //   paged_tile_kernel, 128 rows (prompts and their chunks): bound by the wavefronts' own chain of reads, products, powers and products (at two wavefronts to a SIMD, which the output's registers
 //   allow at 128 dimensions, no unit is full: vector instructions 60 % of the time, LDS 50, the matrix pipes 42).
