@@ -686,3 +686,55 @@ def test_chunks_give_what_a_whole_prompt_gives(S):
     w.k, w.v = held[:2]
     _, bound, _ = w.attention(host(turned), 0.125)
     within(np.concatenate(outs), whole, 2 * bound)
+
+
+def test_calls_that_overlap_and_calls_of_high_priority(S):
+    """Steps of two caches on two streams at once, each with its own workspace, one of them at high priority, give the bits of calls one by one."""
+    torch = S.torch
+    r = np.random.default_rng(44)
+    worlds = [World(S, 45, [1] * 6, [3000, 70, 900, 2, 1500, 64], 2, 4, 128, 64, True).on_gpu(), World(S, 46, [300, 1, 77], [700, 2000, 0], 2, 4, 128, 64, False).on_gpu()]
+    w = dev(S, r.integers(-127, 128, (1536, 1024)).astype(np.int8))
+    ws = dev(S, np.full(1536, 1e-4, np.float32))
+
+    def step(world, x, hp, stream):
+        codes, scale = S.k_quantize_rows(x, hp=hp, stream=stream)
+        qkv = S.k_gemm_i8(codes, scale, w, ws, hp=hp, stream=stream)
+        q = S.k_kv_append(world.cache, world.batch, qkv[:, 1024:1280], qkv[:, 1280:], q=qkv[:, :1024], rope=rope, hp=hp, stream=stream)
+        return S.k_attention_paged(q, world.cache, world.batch, 0.09, hp=hp, stream=stream)
+
+    rope = dev(S, S.rope_table(4096, 128))
+    xs = [dev(S, r.standard_normal((a.tokens, 1024)).astype(np.float16)) for a in worlds]
+    # (appending the same step again leaves a page's scale as it is: the caches are the same from the second step on)
+    want = [[step(a, x, 0, None) for _ in range(2)][1].clone() for a, x in zip(worlds, xs)]
+    streams = [torch.cuda.Stream() for _ in worlds]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(4):
+        for i, (a, x) in enumerate(zip(worlds, xs)):
+            got[i].append(step(a, x, i, streams[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(y, want[i]) for y in got[i]), i
+
+
+@pytest.mark.parametrize("i8", [False, True], ids=["fp16", "int8"])
+def test_prompts_replayed_from_two_graphs(S, i8):
+    """Two captured steps of prompts and single tokens, replayed in turn with other work between: the bits of the eager calls each time."""
+    torch = S.torch
+    worlds = [World(S, 47 + k, new, past, 8, 1, 64, 32, i8).on_gpu() for k, (new, past) in enumerate([([700] + [1] * 12, [900] + [2000 - i for i in range(12)]), ([257, 300], [0, 31])])]
+    xs = [dev(S, (w.r.standard_normal((w.tokens, 512)) * 2).astype(np.float16)) for w in worlds]
+    want = [S.k_attention_paged(x, w.cache, w.batch, 0.125, 200, 3).clone() for x, w in zip(xs, worlds)]
+    graphs, got = [], []
+    torch.cuda.synchronize()
+    for x, w in zip(xs, worlds):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            got.append(S.k_attention_paged(x, w.cache, w.batch, 0.125, 200, 3))
+        graphs.append(g)
+    for _ in range(3):
+        for g, y in zip(graphs, got):
+            y.zero_()
+            g.replay()
+        S.k_attention_paged(xs[0], worlds[0].cache, worlds[0].batch, 0.3)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
