@@ -58,6 +58,9 @@ __device__ __forceinline__ half2_t two_codes(unsigned a, unsigned b, unsigned se
     return __builtin_elementwise_fma(u, by, off);
 }
 
+// A sum of probabilities as they were rounded, so that a key which takes nearly all gives its value, whatever its probability was rounded to
+__device__ __forceinline__ float plus_both(float sum, half2_t p) { return __builtin_amdgcn_fdot2(p, half2_t{(half_t)1.f, (half_t)1.f}, sum, false); }
+
 // The blocks of keys that any of the positions lo .. hi sees, in order: the first `sink` ones, then those from `from` on, `count` in all.
 struct Blocks {
     int sink, from, count;
@@ -268,10 +271,11 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_stream_kernel(const
             }
             const float ref = m[x] > -INFINITY ? m[x] : 0.f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float v = __builtin_amdgcn_exp2f(sc[e] - ref);
-                l[x] += v;
-                pf[x][e] = (half_t)v;
+            for (int e = 0; e < 8; e += 2) {
+                const half2_t y = {(half_t)__builtin_amdgcn_exp2f(sc[e] - ref), (half_t)__builtin_amdgcn_exp2f(sc[e + 1] - ref)};
+                l[x] = plus_both(l[x], y);
+                pf[x][e] = y[0];
+                pf[x][e + 1] = y[1];
             }
         }
         keys_done();
@@ -478,11 +482,12 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
     const int ptid = I8 ? (tid & ~12) | (tid & 4) << 1 | (tid & 8) >> 1 : tid;
     uintx4 raw[NI];
     // A lane of each wavefront holds what is to be known of a block: where it begins (behind all rows: not seen) and lies in the cache, and its scales; masks say
-    // which of the 64 blocks all of the wavefront's rows see whole, and of which each key is seen by some row of the tile.
+    // which of the 64 blocks all of the wavefront's rows see whole, of which each key is seen by some row of the tile, and of which the rest of the values'
+    // scale is below 1.
     int k0s = 0;
     unsigned from_lo = 0, from_hi = 0;
     float kcs = c, vpow = 1.f, vlog = 0.f, vinv = 1.f;
-    unsigned long long full = 0, open = 0;
+    unsigned long long full = 0, open = 0, tiny = 0;
     auto look_up = [&](int first) __attribute__((always_inline)) {
         k0s = NOWHERE;
         from_lo = from_hi = 0;
@@ -508,7 +513,8 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
             }
         }
         full = __ballot(k0s + KEYS - 1 <= lo && (!p.window || hi - k0s < p.window || k0s + KEYS - 1 < p.sinks));
-        if (!I8) open = __ballot(k0s + KEYS - 1 <= t.hi && (!p.window || t.lo - k0s < p.window || k0s + KEYS - 1 < p.sinks));
+        if (I8) tiny = __ballot(vinv > 1.f);
+        else open = __ballot(k0s + KEYS - 1 <= t.hi && (!p.window || t.lo - k0s < p.window || k0s + KEYS - 1 < p.sinks));
     };
     auto of_block = [](int v, int n) __attribute__((always_inline)) { return __builtin_amdgcn_readlane(v, n); };
     auto of_blockf = [](float v, int n) __attribute__((always_inline)) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), n)); };
@@ -623,10 +629,18 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
         const float ref = m > -INFINITY ? m : 0.f;
         // four steps of 16 keys each
         half8 pf[2], vf[D / 32];
-        float off[2], sum[2] = {0.f, 0.f};
+        float off[2], sum[2] = {0.f, 0.f}, exact[2] = {-1.f, -1.f};
         unsigned vbase[D / 32];
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) off[kb] = (I8 ? of_blockf(vlog, n + kb) : 0.f) - ref;
+        if (I8 && (tiny >> n & 3)) {                   // (with the rest of such a scale in them, probabilities may leave nothing in fp16: summed before they are rounded)
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+                exact[kb] = 0.f;
+#pragma unroll
+                for (int v = 0; v < 16; ++v) exact[kb] += __builtin_amdgcn_exp2f(__builtin_fmaf(sc[kb][v], kc[kb], off[kb]));
+            }
+        }
 #pragma unroll
         for (int db = 0; db < D / 32; ++db) {
             vbase[db] = vaddr[db] + (unsigned)(st * STAGE);
@@ -644,10 +658,11 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
             asm volatile("" : "+v"(x), "+v"(y));
             x = __builtin_amdgcn_exp2f(__builtin_fmaf(x, kc[kb], off[kb]));
             y = __builtin_amdgcn_exp2f(__builtin_fmaf(y, kc[kb], off[kb]));
-            sum[kb] += x + y;
+            const half2_t both = {(half_t)x, (half_t)y};
+            sum[kb] = plus_both(sum[kb], both);
             asm volatile("" : "+v"(sum[kb]));
-            pf[step & 1][j] = (half_t)x;
-            pf[step & 1][j + 1] = (half_t)y;
+            pf[step & 1][j] = both[0];
+            pf[step & 1][j + 1] = both[1];
         };
 #pragma unroll
         for (int db = 0; db < D / 32; ++db) read_values(0, db);
@@ -669,7 +684,7 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
                 __builtin_amdgcn_sched_barrier(0);
             }
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) l = I8 ? __builtin_fmaf(sum[kb], of_blockf(vinv, n + kb), l) : l + sum[kb];
+        for (int kb = 0; kb < 2; ++kb) l = I8 ? __builtin_fmaf(exact[kb] < 0.f ? sum[kb] : exact[kb], of_blockf(vinv, n + kb), l) : l + sum[kb];
     };
 
     // 64 blocks that are looked up at once: two of them in LDS and worked on, two in registers on their way there, two more requested once these are written

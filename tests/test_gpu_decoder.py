@@ -540,6 +540,27 @@ def test_attention_paged_joins_tokens_by_their_sequences_or_as_they_come(S, i8, 
     check_attention(S, World(S, 43, new, past, 8, 1, 64, 64, i8))
 
 
+@pytest.mark.parametrize("i8", [False, True], ids=["fp16", "int8"])
+@pytest.mark.parametrize("new", [1, 150])
+@pytest.mark.parametrize("far", [12, 16, 20])
+def test_attention_paged_many_keys_of_tiny_probabilities(S, new, far, i8):
+    """One key in front of thousands whose probabilities are 2^-far of its own, below the normal numbers of fp16 among them: together they count."""
+    w = World(S, 48, [new], [6000], 1, 1, 64, 64, i8, spare=0)
+    w.k[:] = 0
+    first = w.table[0, 0]
+    if i8:
+        w.ks[:] = 1.0
+        w.k[first, 0, 5, 0] = far
+    else:
+        w.k[first, 0, 5, 0] = far
+    # (scores of 0 and of far * ln 2: q of 1, scale ln 2)
+    q = np.zeros((w.tokens, 64), np.float16)
+    q[:, 0] = 1
+    w.on_gpu()
+    want, bound, rows = w.attention(q, float(np.log(2.0)))
+    within(host(S.k_attention_paged(dev(S, q), w.cache, w.batch, float(np.log(2.0)))), want, bound)
+
+
 def test_attention_paged_shared_pages_and_strided_queries(S):
     """Two sequences that read the same prompt's pages, and queries that are columns of a wider tensor; another scale."""
     for i8 in (False, True):
