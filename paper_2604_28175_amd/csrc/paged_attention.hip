@@ -24,13 +24,13 @@
 //   - 64 keys at a time go through LDS, which holds them twice as fp16: two blocks are worked on, the next two become fp16 on their way from registers to LDS, once
 //     for all four wavefronts, and the two after them are on their way from memory;
 //   - a wavefront issues in order, so its products and its vector instructions are woven by hand: the way to LDS between the products of the scores, a step's powers between
-//     the products that the step before it goes into (254 -> 243 us and 68 -> 63 us in the calls below; blocks that none of a wavefront's rows see are worked on all the same, which costs nothing: the others are waited for);
+//     the products that the step before it goes into (254 -> 243 us and 68 -> 63 us in the calls below; blocks that none
+//     of a wavefront's rows see are worked on all the same, which costs nothing: the others are waited for);
 //   - scores^T with v_mfma_f32_32x32x16_f16, a row to a lane and its partner 32 lanes on; V^T's operands come from LDS transposed (ds_read_b64_tr_b16);
 //   - an int8 value's power of two is its page's, exact in fp16, and the rest of the page's scale goes into the probabilities (see look_up).
 //   Four chunks of 1200 to 2048 tokens behind up to 2048, 8 heads of 128 for 32, int8: 243 us, 755 TFLOP/s of what the masks leave; five of 333 to 4001 with a window of 1024, 12 heads
 //   of 64, fp16: 63 us, 482 TFLOP/s.
 #include <algorithm>
-#include <type_traits>
 
 #include "decoder.hpp"
 
