@@ -759,3 +759,24 @@ def test_prompts_replayed_from_two_graphs(S, i8):
         S.k_attention_paged(xs[0], worlds[0].cache, worlds[0].batch, 0.3)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_outputs_of_another_stream_do_not_lie_where_the_current_one_still_writes(S):
+    """The current stream has work queued on memory that is free again; a call on another stream, which waits for none of it, makes its outputs elsewhere."""
+    torch = S.torch
+    r = np.random.default_rng(49)
+    x, w = (dev(S, r.integers(-127, 128, (n, 64)).astype(np.int8)) for n in (4096, 4096))
+    s = dev(S, np.full(4096, 0.01, np.float32))
+    want = S.k_gemm_i8(x, s, w, s).clone()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    for _ in range(3):
+        old = torch.empty(4096, 4096, dtype=torch.float16, device="cuda")
+        for _ in range(100):
+            old.fill_(7.0)
+        del old
+        y = S.k_gemm_i8(x, s, w, s, stream=side)
+        torch.cuda.synchronize()
+        assert torch.equal(y, want)
+        del y
