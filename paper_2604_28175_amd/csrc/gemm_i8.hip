@@ -109,40 +109,42 @@ __global__ void __launch_bounds__(64 * STREAM_WAVES) gemm_i8_stream_kernel(const
 struct TileArgs { GemmI8 g; TileOrder order; };
 
 constexpr int SLICE = 128;               // of the reduction, a whole cache line of each row
-template <int BM, int BN, int WGM, int WGN, int STAGES>
+template <int BM, int BN, int STAGES, int G>
 constexpr unsigned tile_lds() {
-    const unsigned ring = STAGES * (BM + BN) * SLICE, out = BM * (BN + 8) * 2;
-    return ring > out ? ring : out;
+    const unsigned ring = G * STAGES * (BM + BN) * SLICE, out = BM * (BN + 8) * 2, parts = G > 1 ? BM * (BN + 4) * 4 : 0;
+    return ring > out ? (ring > parts ? ring : parts) : (out > parts ? out : parts);
 }
-template <int BM, int BN, int WGM, int WGN, int STAGES>
-constexpr unsigned tile_lds_all() { return tile_lds<BM, BN, WGM, WGN, STAGES>() + BN * 8; }      // + the channels' scales and biases
-template <int BM, int BN, int WGM, int WGN, int STAGES>
+template <int BM, int BN, int STAGES, int G>
+constexpr unsigned tile_lds_all() { return tile_lds<BM, BN, STAGES, G>() + BN * 8; }      // + the channels' scales and biases
+template <int BM, int BN, int WAVES, int STAGES, int G>
 constexpr int tile_waves_per_simd() {
-    const int w = 160 * 1024 / (int)tile_lds_all<BM, BN, WGM, WGN, STAGES>() * WGM * WGN / 4;
+    const int w = 160 * 1024 / (int)tile_lds_all<BM, BN, STAGES, G>() * WAVES * G / 4;
     return w < 1 ? 1 : w > 4 ? 4 : w;
 }
 
-template <int BM, int BN, int WGM, int WGN, int STAGES>
-__global__ void __launch_bounds__(64 * WGM * WGN, (tile_waves_per_simd<BM, BN, WGM, WGN, STAGES>())) gemm_i8_tile_kernel(const TileArgs a) {
+// G > 1: so many sets of wavefronts, each with a ring of its own, take every G-th slice; their sums meet in LDS.
+template <int BM, int BN, int WGM, int WGN, int STAGES, int G>
+__global__ void __launch_bounds__(64 * WGM * WGN * G, (tile_waves_per_simd<BM, BN, WGM * WGN, STAGES, G>())) gemm_i8_tile_kernel(const TileArgs a) {
     const GemmI8& p = a.g;
-    constexpr int NW = WGM * WGN, NT = 64 * NW;
+    constexpr int NW = WGM * WGN, NT = 64 * NW * G;
     constexpr int TM = BM / WGM, TN = BN / WGN, TMB = TM / 32, TNB = TN / 32, KS = SLICE / 32;
     constexpr int XI = BM / (8 * NW), WI = BN / (8 * NW), NX = XI + WI, NM = TMB * TNB;      // transfers of 8 rows per wavefront and slice; MFMAs per step
     constexpr unsigned STAGE = (BM + BN) * SLICE;
     constexpr int LDC = BN + 8;
-    static_assert(TM % 32 == 0 && TN % 32 == 0 && BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && NW % 2 == 0 && STAGES >= 2 && tile_lds_all<BM, BN, WGM, WGN, STAGES>() <= 160 * 1024, "tile");
+    static_assert(TM % 32 == 0 && TN % 32 == 0 && BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && NW % 2 == 0 && STAGES >= 2 && tile_lds_all<BM, BN, STAGES, G>() <= 160 * 1024, "tile");
 
     extern __shared__ __attribute__((aligned(1024))) char tile_smem[];
     if (p.hp) __builtin_amdgcn_s_setprio(3);
-    const unsigned lds0 = (unsigned)(uintptr_t)tile_smem;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, lh = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, nth = __builtin_amdgcn_readfirstlane(tid >> 6), set = nth / NW, wave = nth % NW, l32 = lane & 31, lh = lane >> 5;
+    const char* const ring = tile_smem + set * (int)(STAGES * STAGE);
+    const unsigned lds0 = (unsigned)(uintptr_t)ring;
     const int wm0 = (wave % WGM) * TM, wn0 = (wave / WGM) * TN;
     int tm, tn;
     place_tile(a.order, xcd_range(a.order.tiles, blockIdx.x), tm, tn);
     const int m0 = tm * BM, n0 = tn * BN;
 
     // the channels' scales and biases lie behind the ring (zeros past the end)
-    float* const channels = (float*)(tile_smem + tile_lds<BM, BN, WGM, WGN, STAGES>());
+    float* const channels = (float*)(tile_smem + tile_lds<BM, BN, STAGES, G>());
     for (int i = tid; i < BN; i += NT) {
         channels[i] = n0 + i < p.N ? p.ws[n0 + i] : 0.f;
         channels[BN + i] = p.bias && n0 + i < p.N ? p.bias[n0 + i] : 0.f;
@@ -181,8 +183,9 @@ __global__ void __launch_bounds__(64 * WGM * WGN, (tile_waves_per_simd<BM, BN, W
     for (int j = 0; j < XI; ++j) xoff[j] = m0 + (j * NW + wave) * 8 + rsub < p.M ? (unsigned)((j * NW + wave) * 8 + rsub) * (unsigned)p.K + cl * 16 : OOB_OFFSET;
 #pragma unroll
     for (int j = 0; j < WI; ++j) woff[j] = n0 + (j * NW + wave) * 8 + rsub < p.N ? (unsigned)((j * NW + wave) * 8 + rsub) * (unsigned)p.K + cl * 16 : OOB_OFFSET;
-    const int nk = (p.K + SLICE - 1) / SLICE;
-    auto issue_one = [&](int stage, int slice, int j) __attribute__((always_inline)) {
+    const int nk = (p.K + G * SLICE - 1) / (G * SLICE);
+    auto issue_one = [&](int stage, int nth_slice, int j) __attribute__((always_inline)) {
+        const int slice = nth_slice * G + set;
         const bool there = slice * SLICE + cl * 16 < p.K;          // (the last slice may be ragged)
         const unsigned at = lds0 + (unsigned)stage * STAGE;
         if (j < XI) dma16(xrsrc, there ? xoff[j] : OOB_OFFSET, (unsigned)(slice * SLICE), at + (unsigned)((j * NW + wave) * 1024));
@@ -191,7 +194,7 @@ __global__ void __launch_bounds__(64 * WGM * WGN, (tile_waves_per_simd<BM, BN, W
     intx16 acc[TNB][TMB] = {};
     intx4 wf[2][TNB], xf[2][TMB];
     auto load_frags = [&](int buf, int stage, int ks) __attribute__((always_inline)) {
-        const char* xs = tile_smem + stage * (int)STAGE;
+        const char* xs = ring + stage * (int)STAGE;
         const char* ws = xs + BM * SLICE;
         const int pos = ((ks * 2 + lh) ^ ((l32 >> 1) & 7)) * 16;
 #pragma unroll
@@ -233,6 +236,30 @@ __global__ void __launch_bounds__(64 * WGM * WGN, (tile_waves_per_simd<BM, BN, W
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");   // the zeros past the end have arrived: LDS is free
 
+    if (G > 1) {                                       // the sets' sums become the first one's
+        int* const parts = (int*)tile_smem;
+        auto each = [&](auto body) __attribute__((always_inline)) {
+#pragma unroll
+            for (int b = 0; b < TMB; ++b)
+#pragma unroll
+                for (int t = 0; t < TNB; ++t)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) body(acc[t][b], 4 * g, (intx4*)(parts + (wm0 + b * 32 + l32) * (BN + 4) + wn0 + t * 32 + 8 * g + 4 * lh));
+        };
+#pragma unroll
+        for (int other = 1; other < G; ++other) {
+            if (set == other) each([](intx16& sum, int v, intx4* at) __attribute__((always_inline)) { *at = intx4{sum[v], sum[v + 1], sum[v + 2], sum[v + 3]}; });
+            __syncthreads();
+            if (set == 0)
+                each([](intx16& sum, int v, intx4* at) __attribute__((always_inline)) {
+                    const intx4 y = *at;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) sum[v + j] += y[j];
+                });
+            __syncthreads();
+        }
+    }
+
     // ---- epilogue, one for each activation: a lane holds the sums of y[m][n .. n + 3], n at 8 g + 4 lh.  Rows of the result begin at any multiple of its element (N may be odd): 16 bytes at a time
     // all the same, which the memory takes at any address.
     auto epilogue = [&](auto activation) __attribute__((always_inline)) {
@@ -240,6 +267,7 @@ __global__ void __launch_bounds__(64 * WGM * WGN, (tile_waves_per_simd<BM, BN, W
     if (!p.out_f32 && !p.res) {
         // rounded results leave through LDS
         half_t* const out = (half_t*)tile_smem;
+        if (set == 0)
 #pragma unroll
         for (int b = 0; b < TMB; ++b) {
             const int mt = wm0 + b * 32 + l32;
@@ -272,7 +300,7 @@ __global__ void __launch_bounds__(64 * WGM * WGN, (tile_waves_per_simd<BM, BN, W
     // with a residual, or in fp32: the sums go through LDS, 32 rows of each wavefront at a time, and are finished by lanes that lie along a row, 8 outputs each
     int* const sums = (int*)tile_smem;
     constexpr int LDS_N = BN + 4;
-    static_assert(WGM * 32 * LDS_N * 4 <= (int)tile_lds<BM, BN, WGM, WGN, STAGES>() && WGM * 32 % (NT / LANES) == 0, "staging");
+    static_assert(WGM * 32 * LDS_N * 4 <= (int)tile_lds<BM, BN, STAGES, G>() && WGM * 32 % (NT / LANES) == 0, "staging");
 #pragma unroll
     for (int b = 0; b < TMB; ++b) {
         __builtin_amdgcn_sched_barrier(0);             // (nothing of the next 32 rows ahead of these: there are no registers for it)
@@ -281,6 +309,7 @@ __global__ void __launch_bounds__(64 * WGM * WGN, (tile_waves_per_simd<BM, BN, W
         for (int i = 0; i < ROWS; ++i) xs[i] = row_of(b, i) < p.M ? p.xs[row_of(b, i)] : 0.f;
         if (TMB > 1) load_res(b);                      // (on its way while the sums are)
         if (b) __syncthreads();
+        if (set == 0)
 #pragma unroll
         for (int t = 0; t < TNB; ++t)
 #pragma unroll
@@ -326,22 +355,22 @@ __global__ void __launch_bounds__(64 * WGM * WGN, (tile_waves_per_simd<BM, BN, W
     else epilogue(std::integral_constant<int, ACT_NONE>{});
 }
 
-template <int BM, int BN, int WGM, int WGN, int STAGES>
+template <int BM, int BN, int WGM, int WGN, int STAGES, int G = 1>
 static int launch_tile(const GemmI8& p, hipStream_t stream) {
     const long long tiles_m = (p.M + BM - 1LL) / BM, tiles_n = (p.N + BN - 1LL) / BN;
-    if (tiles_m * tiles_n * (WGM * WGN / 4) > MOST_WORKGROUPS) { set_error("gemm_i8: grid too large"); return STRAIT_E_SHAPE; }
+    if (tiles_m * tiles_n * (WGM * WGN * G / 4) > MOST_WORKGROUPS) { set_error("gemm_i8: grid too large"); return STRAIT_E_SHAPE; }
     ConvParams order{};
     set_tile_order(order, tiles_m, (int)tiles_n, BM, BN, SLICE, 1);
     const TileArgs a{p, order.order};
-    constexpr unsigned lds = tile_lds_all<BM, BN, WGM, WGN, STAGES>();
-    auto kernel = gemm_i8_tile_kernel<BM, BN, WGM, WGN, STAGES>;
+    constexpr unsigned lds = tile_lds_all<BM, BN, STAGES, G>();
+    auto kernel = gemm_i8_tile_kernel<BM, BN, WGM, WGN, STAGES, G>;
     static std::atomic<bool> configured{false};        // (per tile; setting the attribute twice is harmless)
     if (lds > 64 * 1024 && !configured.load(std::memory_order_acquire)) {
         const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e != hipSuccess) { set_error("gemm_i8: cannot reserve %u bytes of LDS: %s", lds, hipGetErrorString(e)); return STRAIT_E_HIP; }
         configured.store(true, std::memory_order_release);
     }
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(tiles_m * tiles_n)), dim3(64 * WGM * WGN), lds, stream, a);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(tiles_m * tiles_n)), dim3(64 * WGM * WGN * G), lds, stream, a);
     return 0;
 }
 template <int MT, int NT, int STEPS>
@@ -359,6 +388,9 @@ static int launch_stream(const GemmI8& p, hipStream_t stream) {
 // More: the tile with the least time for the most tiles that a compute unit gets.  A slice of 128 takes a unit 0.24 us on a 64 x 64 tile, 0.66 on 128 x 128, 1.11 on 256 x 128
 // and 2.05 on 256 x 256 with all units at work (256 x 4096 x 4096 12.0, 17.9, 27.0 and 45.1 us; 512 x 5120 x 2048 16.5, 12.8, 17.9 and 28.0; 2048 x 4096 x 4096 62.7, 45.7, 38.3 and 49.6;
 // 4096 x 4096 x 4096 119, 88.2, 75.6 and 68.2; 8192 x 16384 x 4096 1191, 777, 615 and 529).
+// Where one round of small tiles is all there is, a unit's one tile waits for its own transfers and barriers: two sets of wavefronts share out its slices if there are enough of these (64 x 64:
+// 128 x 4096 x 4096 11.2 and 10.1 us, 64 x 4096 x 16384 29.2 and 24.2, 300 x 1024 x 8192 17.5 and 15.0, but 48 x 2304 x 768 4.9 and 5.0, and with two rounds 512 x 4096 x 4096 18.8 and
+// 19.8; 128 x 64 with two sets, 64 x 64 and 128 x 128 without: 512 x 4096 x 4096 16.9, 18.8 and 20.3, 300 x 5120 x 4096 14.8, 16.0 and 18.1, 400 x 4096 x 8192 25.6, 27.8 and 31.1).
 int launch_gemm_i8(const GemmI8& p, hipStream_t stream) {
     int rc = 0;
     if (p.M <= 16) {
@@ -368,16 +400,17 @@ int launch_gemm_i8(const GemmI8& p, hipStream_t stream) {
     } else if (p.M <= 48 && p.N <= 4096 && p.K <= 2048) {
         rc = launch_stream<3, 1, 4>(p, stream);
     } else {
-        const struct { int bm, bn; float us; } tile[4] = {{64, 64, 0.24f}, {128, 128, 0.66f}, {256, 128, 1.11f}, {256, 256, 2.05f}};
+        const struct { int bm, bn; float us; bool two; } tile[6] = {{64, 64, 0.24f, false}, {128, 128, 0.66f, false}, {256, 128, 1.11f, false}, {256, 256, 2.05f, false}, {64, 64, 0.21f, true}, {128, 64, 0.36f, true}};
         int best = 0;
         float least = 0.f;
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 6; ++i) {
             const long long tiles = (p.M + tile[i].bm - 1LL) / tile[i].bm * ((p.N + tile[i].bn - 1LL) / tile[i].bn);
+            if (tile[i].two && (tiles > 256 || p.K <= 2048)) continue;
             const float us = (float)((tiles + 255) / 256) * tile[i].us;
             if (!i || us < least) { best = i; least = us; }
         }
         rc = best == 0 ? launch_tile<64, 64, 2, 2, 4>(p, stream) : best == 1 ? launch_tile<128, 128, 4, 2, 4>(p, stream) : best == 2 ? launch_tile<256, 128, 4, 2, 3>(p, stream)
-                                                                                                                         : launch_tile<256, 256, 2, 4, 2>(p, stream);
+             : best == 3 ? launch_tile<256, 256, 2, 4, 2>(p, stream) : best == 4 ? launch_tile<64, 64, 2, 2, 4, 2>(p, stream) : launch_tile<128, 64, 4, 2, 3, 2>(p, stream);
     }
     if (rc) return rc;
     hipError_t e = hipGetLastError();

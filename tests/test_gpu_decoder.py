@@ -113,6 +113,21 @@ def test_gemm_i8(S, case):
     within(host(y), *gemm_bound(x, xs, w, ws, bias, res, act, out_f32), f"gemm_i8 {case}")
 
 
+SHARED = [  # slices of a tile that two sets of wavefronts share out: odd and even numbers of them, ragged ends, each epilogue
+    (20, 100, 131056, 0, False, True, True), (50, 64, 2064, 3, True, False, True), (64, 4099, 2176, 0, True, True, False), (200, 513, 2304, 2, False, False, True), (256, 4096, 4096, 0, False, False, True),
+    (300, 4100, 2096, 0, True, False, True), (290, 4161, 2192, 3, False, False, False), (385, 4096, 2320, 1, True, True, True), (300, 5003, 4096, 0, True, False, True),
+]
+
+
+@pytest.mark.parametrize("case", SHARED, ids=lambda c: "x".join(map(str, c[:3])))
+def test_gemm_i8_with_slices_shared_out(S, case):
+    M, N, K, act, use_res, out_f32, use_bias = case
+    x, xs, w, ws, bias, res = product(S, np.random.default_rng(M + N + K), M, N, K, act, use_res, out_f32, use_bias)
+    y = S.k_gemm_i8(dev(S, x), dev(S, xs), dev(S, w), dev(S, ws), dev(S, bias), act, dev(S, res), out_f32)
+    want, bound = gemm_bound(x, xs, w, ws, bias, res, act, out_f32)
+    within(host(y), want, bound)
+
+
 def test_gemm_i8_rows_have_the_same_bits_in_every_batch(S):
     r = np.random.default_rng(3)
     x, xs, w, ws, bias, res = (dev(S, a) for a in product(S, r, 1300, 520, 784, 3, True, False, True))
