@@ -9,7 +9,7 @@
 //   once on the whole chip.  The partial sums meet in LDS as integers.  1 x 4096 x 4096 6.2 us (2.7 TB/s), 16 x 16384 x 4096 13.0 us (5.2 TB/s).
 //
 //   gemm_i8_tile_kernel: bound by the matrix pipes.  Slices of 128 of the reduction travel to a ring in LDS without passing through registers, the operands of
-//   the next MFMAs are read while the current ones run, and one barrier per slice hands a stage on.  8192 x 16384 x 4096 520 to 530 us, 2.1 POP/s, where the library's largest products
+//   the next MFMAs are read while the current ones run, and one barrier per slice hands a stage on.  8192 x 16384 x 4096 500 to 530 us, 2.1 POP/s, where the library's largest products
 //   reach 2.15 and MFMAs on registers alone 2.3: the card's power.  An epilogue for each activation: one that asks at every output took 15 to 20 % of the whole kernel's time.
 #include <type_traits>
 
@@ -135,7 +135,7 @@ __global__ void __launch_bounds__(64 * WGM * WGN * G, (tile_waves_per_simd<BM, B
 
     extern __shared__ __attribute__((aligned(1024))) char tile_smem[];
     if (p.hp) __builtin_amdgcn_s_setprio(3);
-    const int tid = threadIdx.x, lane = tid & 63, nth = __builtin_amdgcn_readfirstlane(tid >> 6), set = nth / NW, wave = nth % NW, l32 = lane & 31, lh = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, nth = __builtin_amdgcn_readfirstlane(tid >> 6), set = G > 1 ? nth / NW : 0, wave = G > 1 ? nth % NW : nth, l32 = lane & 31, lh = lane >> 5;
     const char* const ring = tile_smem + set * (int)(STAGES * STAGE);
     const unsigned lds0 = (unsigned)(uintptr_t)ring;
     const int wm0 = (wave % WGM) * TM, wn0 = (wave / WGM) * TN;
