@@ -6,7 +6,7 @@
 // 32 that lie on one page each.  One pass with a running maximum, which follows the true one only where that is more than 8 (in log2) ahead: probabilities stay below 2^8, and
 // the output is rescaled a few times in all.  Scores, statistics and outputs are fp32; the probabilities are rounded to fp16, half a step each, to be an operand of the second product.
 //
-//   paged_stream_kernel, 16 or 32 rows (steps of single tokens): bound by the cache's bytes.  Blocks are shared out over workgroups (parts of `per_part` blocks, whose
+//   paged_stream_kernel, tiles of 16 or 32 rows (steps of single tokens, or few): bound by the cache's bytes.  Blocks are shared out over workgroups (parts of `per_part` blocks, whose
 //   results a second launch joins) and over a workgroup's four wavefronts, which take every fourth block and meet only at the end:
 //   - a wavefront's page numbers and scales are fetched at once, a lane for each block, and named by v_readlane; the next block's bytes are on their way to
 //     registers while a block is worked on, and none goes through LDS;
@@ -818,7 +818,8 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const PagedArgs few, co
     *(uint2*)(p.out + ((long long)(s.first + i) * p.heads + hq) * D + d * 4) = *(const uint2*)h;
 }
 
-// How a call is launched.  Sequences with up to 16 or 32 rows of a kv head: the stream kernel, tiles of 16 or 32 rows.  More: the tile kernel, 128 rows, of which a compute unit holds
+// How a call is launched.  Sequences with up to 16 or 32 rows of a kv head: the stream kernel, tiles of 16 or 32 rows, and two of these for 49 to 64 (64 rows: 64 sequences of 950 keys and 8 heads
+// 46 us and on the tile kernel 58, 4 heads 28 and 41, 16 of 3100 and 8 heads 59 and 64, 128 of up to 1000 73 and 68; but of 40 rows 32 sequences of 1200 keys 56 and 47).  More: the tile kernel, 128 rows, of which a compute unit holds
 // two, or three of 64 dimensions.  (256 rows by eight wavefronts fill LDS half as often, but all of them stand at one barrier: chunks of four prompts as fast, with a window a third slower.)  A step of
 // both kinds gets both launches.  Parts of as many blocks as give each compute unit several workgroups (tile kernel: where it would not have one).
 struct PagedPlan { PagedArgs few, many; size_t workspace; long long joins; };
@@ -854,7 +855,7 @@ static PagedPlan paged_plan(const PagedAttention& p) {
     const long long rows = (long long)p.batch.max_q * few.group;
     // (single tokens beside prompts' chunks are worth launches of their own where their caches may be long: taken to be there if the sequences but for the longest bring few tokens)
     const bool singles = p.batch.seqs > 1 && p.batch.tokens - p.batch.max_q <= 128LL * (p.batch.seqs - 1) && p.batch.max_kv > 512;
-    few.to = rows <= 32 ? 32 : few.group > 32 || !singles ? 0 : few.group > 16 ? 32 : 16;
+    few.to = rows <= 32 ? 32 : rows > 48 && rows <= 64 ? 64 : few.group > 32 || !singles ? 0 : few.group > 16 ? 32 : 16;
     few.rows = std::min<long long>(rows, few.to) <= 16 ? 16 : 32;
     r.many.from = few.to; r.many.to = 0x7fffffff; r.many.rows = 128;
     if (few.to) plan_class(few, true);

@@ -428,6 +428,19 @@ def test_attention_paged(S, case, window, sinks, i8):
     check_attention(S, World(S, 21, new, past, H, G, dim, page, i8), window, sinks)
 
 
+TWO_TILES = [  # 49 to 64 rows of a kv head, beside sequences of fewer
+    ([16, 3, 0, 9], [3000, 5, 60, 0], 2, 4, 128, 64), ([1, 1], [700, 40], 1, 64, 64, 32), ([7], [2000], 2, 8, 64, 128), ([13, 13, 1], [90, 0, 4000], 1, 4, 128, 32),
+]
+
+
+@pytest.mark.parametrize("i8", [False, True], ids=["fp16", "int8"])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (70, 40)])
+@pytest.mark.parametrize("case", TWO_TILES, ids=lambda c: f"{len(c[0])}seqs-{max(c[0])}new-{c[3]}group")
+def test_attention_paged_of_two_tiles(S, case, window, sinks, i8):
+    new, past, H, G, dim, page = case
+    check_attention(S, World(S, 50, new, past, H, G, dim, page, i8), window, sinks)
+
+
 UNEVEN = [  # steps of sequences that bring very different numbers of tokens; sequences beyond the 64 that are looked at in one go
     ([300] + [1] * 30, [0] + [i * 17 % 200 for i in range(30)], 2, 1, 64, 32),
     ([1] * 40 + [150] + [2] * 40, [700 + i * 7 % 90 for i in range(40)] + [100] + [i for i in range(40)], 1, 3, 128, 64),
