@@ -391,7 +391,7 @@ strait_status strait_k_argmax_f16(void* stream, const void* x, int32_t rows, int
 
 /* Rows of activations as 8-bit integers with one scale each: s = max |x| * (1 / 127), q = x * (1 / s) rounded to the nearest, ties to even (all in fp32; 0 where s
  * is 0).  x [M] rows of K fp16, `pitch` elements from one to the next (a multiple of 8, >= K; columns of a wider tensor will do); q int8 [M][K]; scale fp32 [M].
- * A row that holds an infinity or a NaN gets the scale NaN and codes of 0, so that a product with it is NaN.  K a multiple of 16 (E_SHAPE); x and q
+ * A row that holds an infinity or a NaN gets the scale NaN and codes of 0, so that a product with it is NaN, whatever its activation.  K a multiple of 16 (E_SHAPE); x and q
  * 16-byte aligned.  M = 0 does nothing. */
 strait_status strait_k_quantize_rows(void* stream, const void* x, int32_t M, int32_t K, int64_t pitch, int8_t* q, float* scale, int32_t hp);
 /* Y[M,N] = act(xs[m] ws[n] sum_k x[m,k] w[n,k] + bias[n] (+ res[m,n])): a product in 8-bit integers with a scale for each token (row of x int8 [M][K]) and

@@ -26,8 +26,12 @@ struct __attribute__((packed, aligned(2))) AnyHalf8 { half8 h; };      // at any
 struct __attribute__((packed, aligned(4))) AnyFloat4 { floatx4 f; };
 
 // One output of a sum: the same operations in the same order in every kernel, so that a row has the same bits whatever launch it is part of.
+// (maximum and minimum: a NaN, which is how a row that was not finite arrives here, stays one in every activation.)
 __device__ __forceinline__ float finish(int sum, float xs, float ws, float bias, float res, int act) {
-    return apply_act(__builtin_fmaf((float)sum, xs * ws, bias) + res, act);
+    const float v = __builtin_fmaf((float)sum, xs * ws, bias) + res;
+    if (act == ACT_RELU) return __builtin_elementwise_maximum(v, 0.f);
+    if (act == ACT_RELU6) return __builtin_elementwise_minimum(__builtin_elementwise_maximum(v, 0.f), 6.f);
+    return apply_act(v, act);
 }
 
 // ---- few rows -------------------------------------------------------------------------------------------------------

@@ -808,3 +808,32 @@ def test_outputs_of_another_stream_do_not_lie_where_the_current_one_still_writes
         torch.cuda.synchronize()
         assert torch.equal(y, want)
         del y
+
+
+@pytest.mark.parametrize("act", [0, 1, 2, 3], ids=["none", "relu", "relu6", "gelu"])
+@pytest.mark.parametrize("use_res,out_f32", [(False, False), (True, False), (False, True)], ids=["plain", "residual", "fp32"])
+@pytest.mark.parametrize("M,N,K", [(3, 70, 48), (20, 300, 512), (40, 300, 512), (70, 5000, 528), (300, 509, 2064), (1500, 2500, 768)], ids=lambda v: str(v))
+def test_gemm_i8_keeps_nan_through_every_activation(S, M, N, K, use_res, out_f32, act):
+    """A row whose scale is NaN, a channel whose bias is, and a residual's element that is: each NaN in the result, and nothing beside them."""
+    x, xs, w, ws, bias, res = product(S, np.random.default_rng(60), M, N, K, act, use_res, out_f32, True)
+    clean = [None if a is None else a.copy() for a in (xs, bias, res)]
+    xs[1], bias[N - 2] = np.nan, np.nan
+    nan = np.zeros((M, N), bool)
+    nan[1], nan[:, N - 2] = True, True
+    if use_res:
+        res[2, 5], nan[2, 5] = np.nan, True
+    y = host(S.k_gemm_i8(dev(S, x), dev(S, xs), dev(S, w), dev(S, ws), dev(S, bias), act, dev(S, res), out_f32))
+    assert np.array_equal(np.isnan(y), nan)
+    want, bound = gemm_bound(x, clean[0], w, ws, clean[1], clean[2], act, out_f32)
+    within(y[~nan], want[~nan], bound[~nan])
+
+
+@pytest.mark.parametrize("act", [0, 1, 2, 3], ids=["none", "relu", "relu6", "gelu"])
+def test_a_row_that_is_not_finite_stays_so_through_a_product(S, act):
+    r = np.random.default_rng(61)
+    for M in (4, 100):
+        x = r.standard_normal((M, 256)).astype(np.float16)
+        x[1, 3], x[2, 200] = np.inf, np.nan
+        w, ws = dev(S, r.integers(-127, 128, (130, 256)).astype(np.int8)), dev(S, np.full(130, 1e-3, np.float32))
+        y = host(S.k_gemm_i8(*S.k_quantize_rows(dev(S, x)), w, ws, act=act))
+        assert np.isnan(y[1:3]).all() and np.isfinite(np.delete(y, [1, 2], 0)).all(), M
