@@ -403,7 +403,7 @@ strait_status strait_k_gemm_i8(void* stream, const int8_t* x, const float* x_sca
 
 /* A paged cache of keys and values: k, v [pages][kv_heads][page_tokens][head_dim], 16-byte aligned.  STRAIT_KV_F16: fp16 (the scales are not
  * looked at).  STRAIT_KV_I8: int8 codes, k_scale, v_scale fp32 [pages][kv_heads]; a code stands for code * scale of its page and head, scales 0 to 4096 (fp16 numbers
- * have 516 at most).  page_tokens 32, 64, 128 or 256; head_dim 64 or 128 (E_SHAPE otherwise).  Neither has to be initialised. */
+ * have 516 at most, rotated ones 730); a scale of NaN is seen in the results of the tokens that see its page.  page_tokens 32, 64, 128 or 256; head_dim 64 or 128 (E_SHAPE otherwise).  Neither has to be initialised. */
 typedef enum { STRAIT_KV_F16 = 0, STRAIT_KV_I8 = 1 } strait_kv_type;
 typedef struct strait_kv_cache {
     void* k;

@@ -500,7 +500,7 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
                 from_lo = (unsigned)from;
                 from_hi = (unsigned)(from >> 32);
                 if (I8) {
-                    kcs = fmaxf(p.cache.k_scale[place] * c, 0x1p-126f);       // (times 0, minus infinity were none)
+                    kcs = __builtin_elementwise_maximum(p.cache.k_scale[place] * c, 0x1p-126f);       // (times 0, minus infinity were none; a NaN stays one)
                     // a value is code 2^f, exact in fp16, f between -24 and 5 (1152 2^f is a number of fp16 too); the rest of its scale, between 1 and 2 for scales of 2^-24 to 64, goes into
                     // the probabilities (128 times 2^8 at most).  Scales below 2^-60, of which no output would show a bit, count as 0: the rest would take the probabilities out of fp32.
                     const float vs = p.cache.v_scale[place] < 0x1p-60f ? 0.f : p.cache.v_scale[place];

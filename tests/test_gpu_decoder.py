@@ -837,3 +837,16 @@ def test_a_row_that_is_not_finite_stays_so_through_a_product(S, act):
         w, ws = dev(S, r.integers(-127, 128, (130, 256)).astype(np.int8)), dev(S, np.full(130, 1e-3, np.float32))
         y = host(S.k_gemm_i8(*S.k_quantize_rows(dev(S, x)), w, ws, act=act))
         assert np.isnan(y[1:3]).all() and np.isfinite(np.delete(y, [1, 2], 0)).all(), M
+
+
+@pytest.mark.parametrize("new,past", [([1], [900]), ([150], [100])], ids=["stream", "tile"])
+@pytest.mark.parametrize("what", ["k", "v"])
+def test_attention_paged_shows_a_scale_of_nan(S, what, new, past):
+    """A page and head whose scale is NaN makes NaN of every token that sees it, whichever kernel has it, and of no other head."""
+    w = World(S, 62, new, past, 2, 2, 64, 32, True)
+    scale = w.ks if what == "k" else w.vs
+    scale[w.table[0, 1], 0] = np.nan
+    w.on_gpu()
+    q = dev(S, (w.r.standard_normal((w.tokens, 4 * 64)) * 2).astype(np.float16))
+    got = host(S.k_attention_paged(q, w.cache, w.batch, 0.125))
+    assert np.isnan(got[:, :128]).all() and np.isfinite(got[:, 128:]).all()
