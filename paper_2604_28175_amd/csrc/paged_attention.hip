@@ -30,6 +30,8 @@
 //   - an int8 value's power of two is its page's, exact in fp16, and the rest of the page's scale goes into the probabilities (see look_up).
 //   Four chunks of 1200 to 2048 tokens behind up to 2048, 8 heads of 128 for 32, int8: 243 us, 755 TFLOP/s of what the masks leave; five of 333 to 4001 with a window of 1024, 12 heads
 //   of 64, fp16: 63 us, 482 TFLOP/s.
+#include <float.h>
+
 #include <algorithm>
 
 #include "decoder.hpp"
@@ -56,6 +58,21 @@ __device__ __forceinline__ half2_t two_codes(unsigned a, unsigned b, unsigned se
     const half2_t u = __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(b, a, sel));
     const half2_t by = {(half_t)32768.f, (half_t)32768.f}, off = {(half_t)-0.25f, (half_t)-0.25f};
     return __builtin_elementwise_fma(u, by, off);
+}
+
+// Probabilities are powers of 2 of score - m, where m is any number that is the same for all of a row's sums.  It is the largest score
+constexpr float UNSEEN = -FLT_MAX;       // (before the first one: no score lies further below it than 0, and minus infinity less this is no NaN)
+constexpr float LEAD = 8.f;              // whenever one is further ahead of it than this.
+// A score is a product, of which m is rounded: a power has to be one of the rounded product too, or for scores of 2^28 and more half a step between them is an overflow.
+// Where m is below this, half a step is nothing, and product and difference may be one fused multiply-add.
+constexpr float LARGE = 0x1p20f;
+// What an int8 page's key scale and the score's scale make: finite and above 0, so that minus infinity stays what it is (a NaN stays one)
+__device__ __forceinline__ float factor(float f) { return __builtin_elementwise_minimum(__builtin_elementwise_maximum(f, 0x1p-126f), FLT_MAX); }
+
+// (not to be contracted with what comes after it)
+__device__ __forceinline__ float rounded_product(float a, float b) {
+#pragma clang fp contract(off)
+    return a * b;
 }
 
 // A sum of probabilities as they were rounded, so that a key which takes nearly all gives its value, whatever its probability was rounded to
@@ -210,12 +227,12 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_stream_kernel(const
     float m[RT], l[RT];
 #pragma unroll
     for (int x = 0; x < RT; ++x) {
-        m[x] = -INFINITY;
+        m[x] = UNSEEN;
         l[x] = 0.f;
 #pragma unroll
         for (int j = 0; j < J; ++j) o[x][j] = floatx4{0.f, 0.f, 0.f, 0.f};
     }
-    const float c = p.scale * 1.44269504088896340736f * (I8 ? 512.f : 1.f);
+    const float c = factor(p.scale * 1.44269504088896340736f);
 
     // whether a row sees the key `off` behind some key of which it is `past` tokens past and which is `sinks` keys in front of the last sink
     const int window = p.window ? p.window : NO_WINDOW;
@@ -248,9 +265,7 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_stream_kernel(const
 #pragma unroll
                 for (int u = 0; u < D / 32; ++u) d = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[kb][u], qf[x][u], d, 0, 0, 0);
 #pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    sc[4 * kb + v] = d[v] * kc;
-                }
+                for (int v = 0; v < 4; ++v) sc[4 * kb + v] = rounded_product(d[v], kc);
             }
             if (mask) {
                 asm volatile("");                      // (a branch: most blocks have nothing to mask)
@@ -260,19 +275,18 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_stream_kernel(const
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) top = fmaxf(top, sc[e]);
-            if (__any(top > m[x] + 8.f)) {
+            if (__any(top - m[x] > LEAD)) {
                 top = fmaxf(top, __shfl_xor(top, 16));
                 top = fmaxf(top, __shfl_xor(top, 32));
-                const float now = fmaxf(m[x], top), alpha = now > -INFINITY ? __builtin_amdgcn_exp2f(m[x] - now) : 1.f;
+                const float now = fmaxf(m[x], top), alpha = __builtin_amdgcn_exp2f(m[x] - now);
                 m[x] = now;
                 l[x] *= alpha;
 #pragma unroll
                 for (int j = 0; j < J; ++j) o[x][j] *= alpha;
             }
-            const float ref = m[x] > -INFINITY ? m[x] : 0.f;
 #pragma unroll
             for (int e = 0; e < 8; e += 2) {
-                const half2_t y = {(half_t)__builtin_amdgcn_exp2f(sc[e] - ref), (half_t)__builtin_amdgcn_exp2f(sc[e + 1] - ref)};
+                const half2_t y = {(half_t)__builtin_amdgcn_exp2f(sc[e] - m[x]), (half_t)__builtin_amdgcn_exp2f(sc[e + 1] - m[x])};
                 l[x] = plus_both(l[x], y);
                 pf[x][e] = y[0];
                 pf[x][e + 1] = y[1];
@@ -321,7 +335,7 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_stream_kernel(const
             const int page = p.batch.page_table[(long long)b * p.batch.table_pitch + k0s / P];
             if ((unsigned)page < (unsigned)p.cache.pages) {
                 places = page * H + h;
-                if (I8) { kcs = p.cache.k_scale[places] * c; vss = p.cache.v_scale[places] * 512.f; }
+                if (I8) { kcs = factor(p.cache.k_scale[places] * 512.f * c); vss = p.cache.v_scale[places] * 512.f; }
             }
         }
         unsigned long long left = __ballot(places >= 0);
@@ -372,7 +386,7 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_stream_kernel(const
 #pragma unroll
         for (int x = 0; x < RT; ++x) {
             const float m2 = sml[slot][16 * x + l16][0], l2 = sml[slot][16 * x + l16][1], now = fmaxf(m[x], m2);
-            const float a1 = m[x] > -INFINITY ? __builtin_amdgcn_exp2f(m[x] - now) : 0.f, a2 = m2 > -INFINITY ? __builtin_amdgcn_exp2f(m2 - now) : 0.f;
+            const float a1 = __builtin_amdgcn_exp2f(m[x] - now), a2 = __builtin_amdgcn_exp2f(m2 - now);
             m[x] = now;
             l[x] = l[x] * a1 + l2 * a2;
             const float* row = so[slot][16 * x + l16];
@@ -471,8 +485,9 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
     for (int db = 0; db < D / 32; ++db)
 #pragma unroll
         for (int v = 0; v < 16; ++v) o[db][v] = 0.f;
-    float m = -INFINITY, l = 0.f;
-    const float c = fmaxf(p.scale * 1.44269504088896340736f, 0x1p-126f);
+    float m = UNSEEN, l = 0.f;
+    bool large = false;                                // of some row's m
+    const float c = factor(p.scale * 1.44269504088896340736f);
 
     // ---- memory -> registers -> LDS.  Chunk q of 16 bytes of row r lies at q ^ (r % 16) for K (D = 64: r / 2 % 8, two rows to the width of the banks), whose operand is 16 rows at one
     // chunk.  V's operand is 4 rows at 4 chunks at a time: the rows' bits go to the chunk's bits above those.  Eight lanes store at a time, and codes go to every second chunk: so that they meet
@@ -500,7 +515,7 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
                 from_lo = (unsigned)from;
                 from_hi = (unsigned)(from >> 32);
                 if (I8) {
-                    kcs = __builtin_elementwise_maximum(p.cache.k_scale[place] * c, 0x1p-126f);       // (times 0, minus infinity were none; a NaN stays one)
+                    kcs = factor(p.cache.k_scale[place] * c);
                     // a value is code 2^f, exact in fp16, f between -24 and 5 (1152 2^f is a number of fp16 too); the rest of its scale, between 1 and 2 for scales of 2^-24 to 64, goes into
                     // the probabilities (128 times 2^8 at most).  Scales below 2^-60, of which no output would show a bit, count as 0: the rest would take the probabilities out of fp32.
                     const float vs = p.cache.v_scale[place] < 0x1p-60f ? 0.f : p.cache.v_scale[place];
@@ -579,7 +594,7 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
     auto work = [&](int n, int st, bool mask, auto scores_done) __attribute__((always_inline)) {
         const char* ks0 = tile_lds + st * STAGE;
         floatx16 sc[2];                                // lane holds its row against keys 32 kb + 8 g + 4 lh + j of the tile (v = 4 g + j)
-        float kc[2], top = -INFINITY;
+        float kc[2], most[2];
         half8 kf[D / 16];
         auto read_key = [&](int kb, int ks) __attribute__((always_inline)) { kf[ks] = *(const half8*)(ks0 + (kb * 32 + l32) * ROW + (((ks * 2 + lh) ^ kswz(l32)) << 4)); };
 #pragma unroll
@@ -610,15 +625,15 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
 #pragma unroll
                 for (int v = 0; v < 16; ++v) sc[kb][v] = sees(8 * (v >> 2) + (v & 3), pos - k0 - 4 * lh, p.sinks - k0 - 4 * lh) ? sc[kb][v] : -INFINITY;
             }
-            float most = sc[kb][0];
+            most[kb] = sc[kb][0];
 #pragma unroll
-            for (int v = 1; v < 16; ++v) most = fmaxf(most, sc[kb][v]);
-            top = fmaxf(top, most * kc[kb]);
+            for (int v = 1; v < 16; ++v) most[kb] = fmaxf(most[kb], sc[kb][v]);
         }
-        if (__any(top > m + 8.f)) {
-            const float2 both = halves_of(top);
-            const float now = fmaxf(m, fmaxf(both.x, both.y)), alpha = now > -INFINITY ? __builtin_amdgcn_exp2f(m - now) : 1.f;
+        if (__any(fmaxf(__builtin_fmaf(most[0], kc[0], -m), __builtin_fmaf(most[1], kc[1], -m)) > LEAD)) {
+            const float2 both = halves_of(fmaxf(most[0] * kc[0], most[1] * kc[1]));
+            const float now = fmaxf(m, fmaxf(both.x, both.y)), alpha = __builtin_amdgcn_exp2f(m - now);
             m = now;
+            large = __any(fabsf(m) > LARGE && m != UNSEEN);
             l *= alpha;
 #pragma unroll
             for (int db = 0; db < D / 32; ++db)
@@ -626,13 +641,22 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
                 for (int v = 0; v < 16; ++v) o[db][v] *= alpha;
         }
         __builtin_amdgcn_sched_barrier(0);
-        const float ref = m > -INFINITY ? m : 0.f;
         // four steps of 16 keys each
         half8 pf[2], vf[D / 32];
         float off[2], sum[2] = {0.f, 0.f}, exact[2] = {-1.f, -1.f};
         unsigned vbase[D / 32];
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) off[kb] = (I8 ? of_blockf(vlog, n + kb) : 0.f) - ref;
+        for (int kb = 0; kb < 2; ++kb) off[kb] = (I8 ? of_blockf(vlog, n + kb) : 0.f) - m;
+        if (large) {                                   // (no power beyond what fp16 holds: off may have lost the page's part of it)
+            asm volatile("");
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+                for (int v = 0; v < 16; ++v) sc[kb][v] = __builtin_elementwise_minimum(rounded_product(sc[kb][v], kc[kb]) + off[kb], 15.f);
+                kc[kb] = 1.f;
+                off[kb] = 0.f;
+            }
+        }
         if (I8 && (tiny >> n & 3)) {                   // (with the rest of such a scale in them, probabilities may leave nothing in fp16: summed before they are rounded)
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) {

@@ -850,3 +850,27 @@ def test_attention_paged_shows_a_scale_of_nan(S, what, new, past):
     q = dev(S, (w.r.standard_normal((w.tokens, 4 * 64)) * 2).astype(np.float16))
     got = host(S.k_attention_paged(q, w.cache, w.batch, 0.125))
     assert np.isnan(got[:, :128]).all() and np.isfinite(got[:, 128:]).all()
+
+
+@pytest.mark.parametrize("i8", [False, True], ids=["fp16", "int8"])
+@pytest.mark.parametrize("new,past", [([1, 1], [900, 4]), ([150, 5], [100, 0]), ([150, 150], [3000, 900])], ids=["stream", "tile", "tile-long"])
+@pytest.mark.parametrize("scale", [1e6, 1e7, 3e8, 1e12, 1e30, 1e36])
+def test_attention_paged_of_very_large_scores(S, scale, new, past, i8):
+    """Scores up to the largest numbers of fp32, where half a step of one is a large number: five equal keys in front share all of the weight."""
+    w = World(S, 63, new, past, 1, 4, 64, 32, i8)
+    w.k[..., 0] = 0
+    q = (w.r.standard_normal((w.tokens, 4 * 64)) * 0.01).astype(np.float16)
+    q.reshape(-1, 64)[:, 0] = 7.3
+    for b in range(2):
+        w.k[w.table[b, 0], :, :5] = 0
+        w.k[w.table[b, 0], :, :5, 0] = 113 if i8 else 3.7
+        w.v[w.table[b, 0], :, :5] = w.v[w.table[b, 0], :, :1]
+    w.on_gpu()
+    got = host(S.k_attention_paged(dev(S, q), w.cache, w.batch, scale))
+    _, v = w.values()
+    q0 = 0
+    for b, n in enumerate(w.new):
+        want = np.broadcast_to(v[w.table[b, 0], 0, 0], (n, 4, 64)).reshape(n, -1)
+        # half a step of the result; a value, if it is rounded, half a step too
+        within(got[q0:q0 + n], want, 2 * HALF16 * 1.001 * np.abs(want) + TINY16 + 64 * HALF32)
+        q0 += n
