@@ -449,7 +449,8 @@ strait_status strait_k_kv_append(void* stream, const strait_kv_cache* cache, con
  * out = sum_j softmax_j(scale q . k_j) v_j over what it sees; a token that sees nothing (at a negative position) gets zeros.  Keys on pages that are not followed count as not seen,
  * and pages of which no token of the step sees a key are not looked at (their numbers may be anything).  What lies in the cache behind a sequence's last token, or in keys that no
  * token of its sequence's step sees, has no effect, be it infinite or NaN; an fp16 value that is infinite or NaN and that only some of a sequence's tokens see may reach the others through a
- * probability of 0.  scale finite and > 0.  window, sinks >= 0.
+ * probability of 0.  Scores and sums are fp32.  Probabilities are fp16, and 0 below 2^-31 of the largest one: of N keys that one sum takes in, far ones lose N 2^-31 of the weight at
+ * most (2^-11 of a million).  scale finite and > 0.  window, sinks >= 0.
  * workspace: strait_k_attention_paged_workspace bytes (which may be 0), 16-byte aligned, used during the call only; calls that overlap need one each. */
 strait_status strait_k_attention_paged_workspace(const strait_kv_cache* cache, const strait_kv_batch* batch, int32_t heads, int32_t window, int32_t sinks, size_t* bytes);
 strait_status strait_k_attention_paged(void* stream, const strait_kv_cache* cache, const strait_kv_batch* batch, const void* q, int64_t pitch_q, int32_t heads,

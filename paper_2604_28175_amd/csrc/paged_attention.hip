@@ -3,8 +3,8 @@
 //   out[t, h] = sum_j softmax_j( scale q[t, h] . k_j ) v_j  over the keys j <= p  with  window == 0  or  p - j < window  or  j < sinks
 //
 // The rows of a tile are (token, head of the group) pairs of one kv head: all of them read the same keys.  The keys that any of them sees come in blocks of
-// 32 that lie on one page each.  One pass with a running maximum, which follows the true one only where that is more than 8 (in log2) ahead: probabilities stay below 2^8, and
-// the output is rescaled a few times in all.  Scores, statistics and outputs are fp32; the probabilities are rounded to fp16, half a step each, to be an operand of the second product.
+// 32 that lie on one page each.  One pass with a running maximum, which follows the true one only where that is more than 8 (in log2) ahead, so that the output is rescaled a few times
+// in all.  Scores, statistics and outputs are fp32; the probabilities are rounded to fp16, half a step each, to be an operand of the second product (2^-32 of the largest one where they are small).
 //
 //   paged_stream_kernel, tiles of 16 or 32 rows (steps of single tokens, or few): bound by the cache's bytes.  Blocks are shared out over workgroups (parts of `per_part` blocks, whose
 //   results a second launch joins) and over a workgroup's four wavefronts, which take every fourth block and meet only at the end:
@@ -60,9 +60,10 @@ __device__ __forceinline__ half2_t two_codes(unsigned a, unsigned b, unsigned se
     return __builtin_elementwise_fma(u, by, off);
 }
 
-// Probabilities are powers of 2 of score - m, where m is any number that is the same for all of a row's sums.  It is the largest score
+// Probabilities are powers of 2 of score - m, where m is any number that is the same for all of a row's sums.  It is the largest score less
+constexpr float ROOM = 7.f;              // (so that the powers use what fp16 holds, up to 2^15: those of far keys become 0 from 2^-32 of the largest one on, not from 2^-25),
 constexpr float UNSEEN = -FLT_MAX;       // (before the first one: no score lies further below it than 0, and minus infinity less this is no NaN)
-constexpr float LEAD = 8.f;              // whenever one is further ahead of it than this.
+constexpr float LEAD = 15.f;             // whenever one is further ahead of it than this.
 // A score is a product, of which m is rounded: a power has to be one of the rounded product too, or for scores of 2^28 and more half a step between them is an overflow.
 // Where m is below this, half a step is nothing, and product and difference may be one fused multiply-add.
 constexpr float LARGE = 0x1p20f;
@@ -278,7 +279,7 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_stream_kernel(const
             if (__any(top - m[x] > LEAD)) {
                 top = fmaxf(top, __shfl_xor(top, 16));
                 top = fmaxf(top, __shfl_xor(top, 32));
-                const float now = fmaxf(m[x], top), alpha = __builtin_amdgcn_exp2f(m[x] - now);
+                const float now = fmaxf(m[x], top - ROOM), alpha = __builtin_amdgcn_exp2f(m[x] - now);
                 m[x] = now;
                 l[x] *= alpha;
 #pragma unroll
@@ -449,6 +450,7 @@ __device__ __forceinline__ float2 halves_of(float v) {
 }
 
 constexpr int TILE_KEYS = 64;            // two blocks
+constexpr float VALUE = 128.f;           // what is left out of the values of an int8 cache until the end
 
 template <int D, bool I8>
 __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const PagedArgs a) {
@@ -516,12 +518,12 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
                 from_hi = (unsigned)(from >> 32);
                 if (I8) {
                     kcs = factor(p.cache.k_scale[place] * c);
-                    // a value is code 2^f, exact in fp16, f between -24 and 5 (1152 2^f is a number of fp16 too); the rest of its scale, between 1 and 2 for scales of 2^-24 to 64, goes into
-                    // the probabilities (128 times 2^8 at most).  Scales below 2^-60, of which no output would show a bit, count as 0: the rest would take the probabilities out of fp32.
+                    // a value is 2^7 code 2^f: code 2^f is exact in fp16, f between -24 and 5 (1152 2^f is a number of fp16 too), and 2^7 comes at the end; the rest of the page's scale, between
+                    // 1 and 2 for scales of 2^-17 to 8192, goes into the powers.  Scales below 2^-60, of which no output would show a bit, count as 0: the rest would take the powers out of fp32.
                     const float vs = p.cache.v_scale[place] < 0x1p-60f ? 0.f : p.cache.v_scale[place];
-                    vpow = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, vs) & 0x7f800000u);
+                    vpow = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, vs) & 0x7f800000u) * (1.f / VALUE);
                     vpow = vs == 0.f ? 0.f : fminf(fmaxf(vpow, 0x1p-24f), 0x1p5f);
-                    const float ratio = vs == 0.f ? 1.f : vs / vpow;
+                    const float ratio = vs == 0.f ? 1.f : vs / (vpow * VALUE);
                     vlog = __builtin_amdgcn_logf(ratio);
                     vinv = 1.f / ratio;
                 }
@@ -629,10 +631,19 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
 #pragma unroll
             for (int v = 1; v < 16; ++v) most[kb] = fmaxf(most[kb], sc[kb][v]);
         }
-        if (__any(fmaxf(__builtin_fmaf(most[0], kc[0], -m), __builtin_fmaf(most[1], kc[1], -m)) > LEAD)) {
-            const float2 both = halves_of(fmaxf(most[0] * kc[0], most[1] * kc[1]));
-            const float now = fmaxf(m, fmaxf(both.x, both.y)), alpha = __builtin_amdgcn_exp2f(m - now);
+        // (what is added to a block's scores; here the scores' maximum is one of the powers' exponents, the rest of a page's scale among them)
+        float rest[2], off[2];
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            rest[kb] = I8 ? of_blockf(vlog, n + kb) : 0.f;
+            off[kb] = rest[kb] - m;
+        }
+        if (__any(fmaxf(__builtin_fmaf(most[0], kc[0], off[0]), __builtin_fmaf(most[1], kc[1], off[1])) > LEAD)) {
+            const float2 both = halves_of(fmaxf(rounded_product(most[0], kc[0]) + rest[0], rounded_product(most[1], kc[1]) + rest[1]));
+            const float now = fmaxf(m, fmaxf(both.x, both.y) - ROOM), alpha = __builtin_amdgcn_exp2f(m - now);
             m = now;
+            off[0] = rest[0] - m;
+            off[1] = rest[1] - m;
             large = __any(fabsf(m) > LARGE && m != UNSEEN);
             l *= alpha;
 #pragma unroll
@@ -643,16 +654,14 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
         __builtin_amdgcn_sched_barrier(0);
         // four steps of 16 keys each
         half8 pf[2], vf[D / 32];
-        float off[2], sum[2] = {0.f, 0.f}, exact[2] = {-1.f, -1.f};
+        float sum[2] = {0.f, 0.f}, exact[2] = {-1.f, -1.f};
         unsigned vbase[D / 32];
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) off[kb] = (I8 ? of_blockf(vlog, n + kb) : 0.f) - m;
         if (large) {                                   // (no power beyond what fp16 holds: off may have lost the page's part of it)
             asm volatile("");
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) {
 #pragma unroll
-                for (int v = 0; v < 16; ++v) sc[kb][v] = __builtin_elementwise_minimum(rounded_product(sc[kb][v], kc[kb]) + off[kb], 15.f);
+                for (int v = 0; v < 16; ++v) sc[kb][v] = __builtin_elementwise_minimum(rounded_product(sc[kb][v], kc[kb]) + off[kb], LEAD);
                 kc[kb] = 1.f;
                 off[kb] = 0.f;
             }
@@ -734,7 +743,7 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) paged_tile_kernel(const P
     const float2 ll = halves_of(l);
     l = ll.x + ll.y;
     if (!any) return;
-    const float inv = l == 0.f ? 0.f : 1.f / l;        // nothing seen: zeros
+    const float inv = l == 0.f ? 0.f : (I8 ? VALUE : 1.f) / l;         // nothing seen: zeros
     const bool whole = blocks.count <= a.per_part;
     if (whole) {
         half_t* out = p.out + ((long long)(token < 0 ? 0 : token) * p.heads + head) * D;

@@ -874,3 +874,51 @@ def test_attention_paged_of_very_large_scores(S, scale, new, past, i8):
         # half a step of the result; a value, if it is rounded, half a step too
         within(got[q0:q0 + n], want, 2 * HALF16 * 1.001 * np.abs(want) + TINY16 + 64 * HALF32)
         q0 += n
+
+
+@pytest.mark.parametrize("i8", [False, True], ids=["fp16", "int8"])
+@pytest.mark.parametrize("dim,far", [(64, 24.4), (128, 25.3), (64, 28.2)])
+@pytest.mark.parametrize("seqs,new,keys", [(1, 4096, 1 << 18), (1, 4096, 3 << 20), (64, 1, 1 << 20)], ids=["tile", "tile-longer", "stream"])
+def test_attention_paged_far_keys_together_keep_their_weight(S, seqs, new, keys, dim, far, i8):
+    """One key of value 1 in front of very many whose probabilities are about 2^-far of its own and whose values are -1: with p of these a token's result is (1 - M) / (1 + M), M = p 2^-far.
+    All of the keys but the first share one page, of which the cache holds little.
+
+    Off by half a step of the result, and, with n of the far keys in one sum beside the near one (a wavefront has all of a tile's, and of a single token's among 64 sequences of 8 heads a
+    32nd at most; where the near key is not, the far ones are the largest):
+    - the far probabilities' half of the smallest number of fp16, 2^-32 of the largest power, in both sums: 2 n 2^-32;
+    - fp32's sums.  A product of matrices adds 16 keys at least to a sum of 1 + M at most and rounds it by a step at most, 2^-23; the sum of probabilities rounds by half a step for each 16 keys
+      of one of two lanes.  Together n (2^-23 / 16 + 2^-24 / 32) = n 2^-24 5 / 32 of the result's denominator;
+    - the scores, `far` times fp32's (D + 8) roundings, in M, twice in the result."""
+    H, P = 8, 256
+    k, v = np.zeros((2, H, P, dim), np.float16), np.full((2, H, P, dim), -1, np.float16)
+    far = float(np.float16(far))
+    k[0, :, 0, 0], v[0, :, 0] = far, 1
+    scales = []
+    if i8:
+        scales = [dev(S, np.full((2, H), s, np.float32)) for s in (far / 100, 0.01)]
+        k, v = (k * (100 / far)).round().astype(np.int8), (v * 100).astype(np.int8)
+    cache = S.KvCache(dev(S, k), dev(S, v), *scales)
+    table = np.ones((seqs, keys // P), np.int32)
+    table[:, 0] = 0
+    batch = S.KvBatch(dev(S, np.arange(seqs + 1, dtype=np.int32) * new), dev(S, np.full(seqs, keys, np.int32)), dev(S, table), new, keys)
+    q = S.torch.zeros(seqs * new, H, dim, dtype=S.torch.float16, device="cuda")
+    q[:, :, 0] = 1
+    got = host(S.k_attention_paged(q.view(seqs * new, H * dim), cache, batch, float(np.log(2.0)))).reshape(seqs * new, -1)
+    p = np.tile(np.arange(keys - new, keys), seqs)[:, None].astype(np.float64)
+    n = p / (32 if new == 1 else 1)
+    M = p * 2.0 ** -far
+    want = np.broadcast_to((1 - M) / (1 + M), got.shape)
+    within(got, want, HALF16 * 1.001 * np.abs(want) + 2 * n * 2.0 ** -32 + n * HALF32 * 5 / 32 + 2 * M * far * (dim + 8) * HALF32 + 64 * HALF32)
+
+
+@pytest.mark.parametrize("scale", [1e-7, 2.0 ** -24 * 1.7, 1e-5, 2.0 ** -17, 2.0 ** -18 * 1.99, 70.0, 511.0, 516.0])
+@pytest.mark.parametrize("new,past", [([1, 1], [900, 3]), ([150, 5], [400, 0])], ids=["stream", "tile"])
+def test_attention_paged_of_small_and_large_values(S, new, past, scale):
+    """All pages' values of one size, and single pages of another."""
+    for few in (None, 1e-9, 0.02, 516.0):
+        w = World(S, 65, new, past, 1, 4, 64, 32, True)
+        w.vs[:] = np.float32(scale) * w.r.uniform(0.6, 1.0, w.vs.shape).astype(np.float32)
+        if few:
+            w.vs[w.table[0, 1::3]] = np.float32(few)
+        check_attention(S, w)
+        check_attention(S, w, 90, 5)
