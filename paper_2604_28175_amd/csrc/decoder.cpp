@@ -49,6 +49,8 @@ int paged_arguments(const char* what, const strait_kv_cache* cache, const strait
     if (int rc = check_batch(what, cache, batch)) return rc;
     if (int rc = check_heads(what, cache, batch, heads)) return rc;
     if (window < 0 || sinks < 0) return invalid(what, "window and sinks are not negative");
+    // (each has a workgroup at least; with fewer of them no product of sizes in the plan leaves its type)
+    if ((long long)batch->seqs * cache->kv_heads > MOST_WORKGROUPS) return shape(what, "grid too large");
     p.cache = *cache;
     p.batch = *batch;
     p.heads = heads;

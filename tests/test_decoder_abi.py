@@ -214,3 +214,15 @@ def test_oracle_append_in_pieces():
             g, row = table[0][t // 32], t % 32
             assert (np.abs(codes[g, :, row] * scale[g][:, None].astype(np.float64) - x[t]) <= 0.5001 * np.maximum(steps[g], scale[g])[:, None]).all()
     assert np.isnan(scale[1]).all()
+
+
+def test_attention_over_more_sequences_than_a_launch_holds_is_refused():
+    """Also where the number of tiles that are found by counting, or a product of sizes, would leave its type."""
+    big = 0x7fffffff
+    need = C.c_size_t(1)
+    for seqs, heads, tokens, max_q, max_kv in ((big, 1, 1000, 1000, 1), (big, 1, 1000, 1000, 1 << 29), (big, 1 << 16, 1, 1, 1 << 29), (big, 1 << 15, 100, 100, 1 << 20), (1 << 30, 1 << 10, 8, 8, 1 << 28),
+                                               (big - 100, 2, 5000, 300, 64)):
+        for kind in (S.KV_F16, S.KV_I8):
+            c, b = cache(type=kind, pages=1, kv_heads=heads), batch(seqs=seqs, tokens=tokens, max_q=max_q, max_kv=max_kv, table_pitch=1 << 24)
+            assert attend(c, b, pq=heads * 128, heads=heads, ws_bytes=1 << 62) == SHAPE, (seqs, heads, tokens, max_q, max_kv)
+            assert S.lib.strait_k_attention_paged_workspace(C.byref(c), C.byref(b), heads, 0, 0, C.byref(need)) == SHAPE and need.value == 0
