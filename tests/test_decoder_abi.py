@@ -226,3 +226,14 @@ def test_attention_over_more_sequences_than_a_launch_holds_is_refused():
             c, b = cache(type=kind, pages=1, kv_heads=heads), batch(seqs=seqs, tokens=tokens, max_q=max_q, max_kv=max_kv, table_pitch=1 << 24)
             assert attend(c, b, pq=heads * 128, heads=heads, ws_bytes=1 << 62) == SHAPE, (seqs, heads, tokens, max_q, max_kv)
             assert S.lib.strait_k_attention_paged_workspace(C.byref(c), C.byref(b), heads, 0, 0, C.byref(need)) == SHAPE and need.value == 0
+
+
+def test_a_workspace_that_is_missing_or_too_small_or_misaligned_is_refused():
+    """One token over a long cache is shared out over parts, so it needs room."""
+    need = C.c_size_t(0)
+    long = batch(seqs=1, tokens=1, max_q=1, max_kv=100000, table_pitch=4000)
+    for kind in (S.KV_F16, S.KV_I8):
+        assert S.lib.strait_k_attention_paged_workspace(C.byref(cache(type=kind)), C.byref(long), 4, 0, 0, C.byref(need)) == OK and need.value > 0
+        assert attend(cache(type=kind), long, ws=None) == NOMEM and "workspace" in S.last_error()
+        assert attend(cache(type=kind), long, ws_bytes=need.value - 1) == NOMEM and attend(cache(type=kind), long, ws_bytes=0) == NOMEM
+        assert attend(cache(type=kind), long, ws=A + 4, ws_bytes=need.value) == INVALID and "workspace" in S.last_error()
