@@ -368,11 +368,16 @@ static int launch_tile(const GemmI8& p, hipStream_t stream) {
     const TileArgs a{p, order.order};
     constexpr unsigned lds = tile_lds_all<BM, BN, STAGES, G>();
     auto kernel = gemm_i8_tile_kernel<BM, BN, WGM, WGN, STAGES, G>;
-    static std::atomic<bool> configured{false};        // (per tile; setting the attribute twice is harmless)
-    if (lds > 64 * 1024 && !configured.load(std::memory_order_acquire)) {
-        const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (lds > 64 * 1024) {                             // asked for once per tile and device (twice is harmless; devices beyond the 64th each time)
+        static std::atomic<unsigned long long> asked{0};
+        int device = 0;
+        hipError_t e = hipGetDevice(&device);
+        const unsigned long long bit = device < 64 ? 1ULL << device : 0;
+        if (e == hipSuccess && !(asked.load(std::memory_order_acquire) & bit)) {
+            e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+            if (e == hipSuccess) asked.fetch_or(bit, std::memory_order_release);
+        }
         if (e != hipSuccess) { set_error("gemm_i8: cannot reserve %u bytes of LDS: %s", lds, hipGetErrorString(e)); return STRAIT_E_HIP; }
-        configured.store(true, std::memory_order_release);
     }
     hipLaunchKernelGGL(kernel, dim3((unsigned)(tiles_m * tiles_n)), dim3(64 * WGM * WGN * G), lds, stream, a);
     return 0;

@@ -1,6 +1,10 @@
 """A decoder's operators at the boundary, without a GPU: what is refused before anything is launched, what does nothing, the rotation table, and the oracle
 against closed forms and the encoder's own attention."""
 import ctypes as C
+import os
+import shutil
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -237,3 +241,32 @@ def test_a_workspace_that_is_missing_or_too_small_or_misaligned_is_refused():
         assert attend(cache(type=kind), long, ws=None) == NOMEM and "workspace" in S.last_error()
         assert attend(cache(type=kind), long, ws_bytes=need.value - 1) == NOMEM and attend(cache(type=kind), long, ws_bytes=0) == NOMEM
         assert attend(cache(type=kind), long, ws=A + 4, ws_bytes=need.value) == INVALID and "workspace" in S.last_error()
+
+
+DEVICES = """
+import ctypes, sys
+recorder = ctypes.CDLL(sys.argv[1], mode=ctypes.RTLD_GLOBAL)          # ahead of the runtime that the library brings along
+sys.path.insert(0, sys.argv[2])
+from paper_2604_28175_amd.binding import lib
+A = 4096
+recorded = lambda what: ctypes.c_int.in_dll(recorder, "recorded_" + what)
+counts = []
+for device in (0, 1, 0, 7, 63, 64, 100, 1, 64):
+    recorded("device").value = device
+    for m, n, k in ((1, 64, 64), (40, 8192, 4096), (128, 4096, 4096), (509, 5003, 2064), (512, 4096, 4096), (512, 5120, 2048), (2048, 4096, 4096), (8192, 16384, 4096)):
+        for res, f32 in ((None, 0), (A, 0), (None, 1)):
+            assert lib.strait_k_gemm_i8(None, A, A, A, A, None, m, n, k, 0, res, A, f32, 0) == 0, lib.strait_last_error()
+    counts.append(recorded("asked").value)
+print(counts, recorded("wide").value, recorded("unasked").value)
+sys.exit(0 if recorded("wide").value > 100 and recorded("unasked").value == 0 and counts[1] == 2 * counts[0] and counts[2] == counts[1] else 1)
+"""
+
+
+@pytest.mark.skipif(shutil.which("gcc") is None, reason="no C compiler")
+def test_lds_beyond_the_default_is_asked_for_on_every_device(tmp_path):
+    """The attribute belongs to a device's copy of a kernel; tests/native/devices_recorder.c stands in for the runtime."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    recorder = str(tmp_path / "recorder.so")
+    subprocess.run(["gcc", "-O1", "-shared", "-fPIC", "-o", recorder, os.path.join(root, "tests", "native", "devices_recorder.c")], check=True)
+    r = subprocess.run([sys.executable, "-c", DEVICES, recorder, root], capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0, r.stdout[-1500:] + r.stderr[-1500:]
