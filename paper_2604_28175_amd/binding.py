@@ -707,6 +707,8 @@ class KvCache:
         _any_dense(k, _INT8 if i8 else _FP16, 4, -1, "k")
         self.device = k.get_device()
         _dense(v, k.dtype, tuple(k.shape), self.device, "v")
+        if not k.numel():
+            _refuse(f"a cache has pages, heads, tokens and dimensions, is {_what(k)}")
         if i8 != (k_scale is not None) or i8 != (v_scale is not None):
             _refuse("an int8 cache has k_scale and v_scale, an fp16 cache none")
         if i8:

@@ -922,3 +922,14 @@ def test_attention_paged_of_small_and_large_values(S, new, past, scale):
             w.vs[w.table[0, 1::3]] = np.float32(few)
         check_attention(S, w)
         check_attention(S, w, 90, 5)
+
+
+def test_a_cache_of_no_dimensions_is_refused(S):
+    torch = S.torch
+    w = World(S, 64, [2], [30], 2, 2, 64, 32, True).on_gpu()
+    half = lambda *s: torch.zeros(s, dtype=torch.float16, device="cuda")
+    for shape in ((4, 2, 32, 0), (4, 0, 32, 64), (4, 2, 0, 64), (0, 2, 32, 64)):
+        for call in (lambda c: S.k_attention_paged(half(2, 256), c, w.batch, 1.0), lambda c: S.k_kv_append(c, w.batch, half(2, 128), half(2, 128)),
+                     lambda c: S.k_kv_append(c, w.batch, half(2, 0), half(2, 0), q=half(2, 128))):
+            with pytest.raises(S.StraitError):
+                call(S.KvCache(half(*shape), half(*shape)))
