@@ -644,6 +644,13 @@ def _handle(device: int, stream) -> int:
     return stream.cuda_stream
 
 
+def _used(stream, *tensors):
+    """What a call on a stream of its own reads or writes: the allocator is told, so that the caller may let go of it at once."""
+    for t in tensors:
+        if t is not None:
+            t.record_stream(stream)
+
+
 def _made(stream, like, *shape, dtype):
     """A tensor that a call makes.  For a stream that is not the current one it is that stream's, so that nothing which the current one has yet to do to freed memory meets the call, and the
     current one, which may read it, is told to the allocator."""
@@ -663,6 +670,8 @@ def k_quantize_rows(x, hp=0, stream=None):
         return _elsewhere(device, k_quantize_rows, x, hp, stream)
     m, k = x.shape
     handle = _handle(device, stream)
+    if stream is not None:
+        _used(stream, x)
     q, scale = _made(stream, x, m, k, dtype=_INT8), _made(stream, x, m, dtype=_FP32)
     _check(lib.strait_k_quantize_rows(handle, x.data_ptr(), m, k, pitch, q.data_ptr(), scale.data_ptr(), hp))
     return q, scale
@@ -686,6 +695,8 @@ def k_gemm_i8(x, x_scale, w, w_scale, bias=None, act=ACT_NONE, res=None, out_f32
     if _device_now() != device:
         return _elsewhere(device, k_gemm_i8, x, x_scale, w, w_scale, bias, act, res, out_f32, hp, stream)
     handle = _handle(device, stream)
+    if stream is not None:
+        _used(stream, x, x_scale, w, w_scale, bias, res)
     y = _made(stream, x, m, n, dtype=_FP32 if out_f32 else _FP16)
     _check(lib.strait_k_gemm_i8(handle, x.data_ptr(), x_scale.data_ptr(), w.data_ptr(), w_scale.data_ptr(), _dev(bias), m, n, k, act, _dev(res), y.data_ptr(), out_f32, hp))
     return y
@@ -788,6 +799,8 @@ def k_kv_append(cache: KvCache, batch: KvBatch, k, v, q=None, rope=None, interle
         _dense(q_out, _FP16, (tokens, heads * dim), device, "q_out")
     elif q is not None:
         q_out = _made(stream, q, tokens, heads * dim, dtype=_FP16)
+    if stream is not None:
+        _used(stream, k, v, q, rope, q_out, cache.k, cache.v, cache.k_scale, cache.v_scale, batch.q_start, batch.kv_len, batch.page_table)
     _check(lib.strait_k_kv_append(handle, cache.ref, batch.ref(tokens), _dev(q), k.data_ptr(), v.data_ptr(), pq, pk, pv, heads, _dev(rope), rope_rows, rope_dim,
                                   interleaved, _dev(q_out), hp))
     return q_out
@@ -811,6 +824,8 @@ def k_attention_paged(q, cache: KvCache, batch: KvBatch, scale: float, window: i
         out = _made(stream, q, tokens, width, dtype=_FP16)
     else:
         _dense(out, _FP16, (tokens, width), device, "out")
+    if stream is not None:
+        _used(stream, q, out, cache.k, cache.v, cache.k_scale, cache.v_scale, batch.q_start, batch.kv_len, batch.page_table)
     need, ws = batch.room(cache, tokens, heads, window, sinks), None
     if need:
         ws = _made(stream, q, need // 2, dtype=_FP16)                  # (of halfs; a multiple of 16 bytes)

@@ -933,3 +933,63 @@ def test_a_cache_of_no_dimensions_is_refused(S):
                      lambda c: S.k_kv_append(c, w.batch, half(2, 0), half(2, 0), q=half(2, 128))):
             with pytest.raises(S.StraitError):
                 call(S.KvCache(half(*shape), half(*shape)))
+
+
+def test_what_a_call_on_another_stream_reads_may_be_let_go_of(S):
+    """Inputs, lengths and page numbers that are the current stream's memory, dropped as soon as the calls on a busy stream are made; the current stream then writes to memory of their sizes."""
+    torch = S.torch
+    r = np.random.default_rng(66)
+    w = World(S, 67, [1] * 64, [i * 9 for i in range(64)], 2, 4, 128, 64, True).on_gpu()
+    c, b = w.cache, w.batch
+    kept = [dev(S, a) for a in (r.standard_normal((64, 1024)).astype(np.float16), r.integers(-127, 128, (1536, 1024)).astype(np.int8), np.full(1536, 1e-4, np.float32), np.ones(1536, np.float32),
+                                S.rope_table(w.max_kv, 128), r.integers(-127, 128, (1024, 1024)).astype(np.int8), np.full(1024, 1e-3, np.float32))]
+    kept += [c.k, c.v, c.k_scale, c.v_scale, b.q_start, b.kv_len, b.page_table]
+
+    def step(stream):
+        x, wq, sq, bias, rope, wo, so, *rest = (t.clone() for t in kept)
+        cache, batch = S.KvCache(*rest[:4]), S.KvBatch(*rest[4:], w.max_q, w.max_kv)
+        del rest
+        if stream is not None:
+            stream.wait_stream(torch.cuda.current_stream())
+        qkv = S.k_gemm_i8(*S.k_quantize_rows(x, stream=stream), wq, sq, bias, stream=stream)
+        q = S.k_kv_append(cache, batch, qkv[:, 1024:1280], qkv[:, 1280:], q=qkv[:, :1024], rope=rope, stream=stream)
+        o = S.k_attention_paged(q, cache, batch, 0.09, stream=stream)
+        return S.k_gemm_i8(*S.k_quantize_rows(o, stream=stream), wo, so, res=x, stream=stream)
+
+    want = step(None).clone()
+    side, busy = torch.cuda.Stream(), torch.empty(1 << 28, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    for _ in range(3):
+        with torch.cuda.stream(side):
+            for _ in range(60):
+                busy.fill_(1)
+        y = step(side)
+        junk = [torch.full((t.numel() * t.element_size(),), 100, dtype=torch.uint8, device="cuda") for t in kept for _ in range(3)]
+        torch.cuda.synchronize()
+        assert torch.equal(y, want)
+        del y, junk
+
+
+def test_a_captured_step_on_two_streams(S):
+    """A capture that goes on to a second stream and back: the same bits on every replay, eager steps between them."""
+    torch = S.torch
+    blocks = [Block(S, 68, 2, 4, 128, i8, 0, 0, [400, 90]) for i8 in (True, True)]
+    r = np.random.default_rng(69)
+    prompts = dev(S, r.standard_normal((430, blocks[0].width)).astype(np.float16))
+    for block in blocks:
+        block.step(prompts, block.batch([350, 80], [350, 80]))
+    x, length = torch.zeros((2, blocks[0].width), dtype=torch.float16, device="cuda"), dev(S, np.array([351, 81], np.int32))
+    batches = [S.KvBatch(dev(S, np.arange(3, dtype=np.int32)), length, block.world.batch.page_table, 1, 400) for block in blocks]
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        side.wait_stream(torch.cuda.current_stream())
+        y1 = blocks[1].step(x, batches[1], stream=side)
+        torch.cuda.current_stream().wait_stream(side)
+    for _ in range(5):
+        x.copy_(dev(S, r.standard_normal((2, blocks[0].width)).astype(np.float16)))
+        y0 = blocks[0].step(x, batches[0])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y0, y1)
+        length += 1
