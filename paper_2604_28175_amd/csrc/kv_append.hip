@@ -245,9 +245,13 @@ int launch_kv_append(const KvAppend& p, hipStream_t stream) {
         g.items = (int)items;
         g.blocks = waves ? (g.items + 3) / 4 : g.items;
     }
-    // A wavefront for each token, or four where the tokens are few or have two pieces for each of their threads (8000 tokens of 384 pieces 27.2 us and 32.5; 4000 of 512 27.8 and
-    // 25.9, 128 of 512 7.6 and 4.4)
-    g.token_threads = p.batch.tokens >= 2048 && (p.heads + (i8 ? 0 : 2 * p.cache.kv_heads)) * p.cache.head_dim / 8 < 512 ? 64 : 256;
+    // A wavefront for each token, or four where the tokens are too few to fill the units (to 8 times a token's pieces, beside an int8 cache's items 10 times), and where each has so many pieces
+    // that its finding does not count.  64 and 256 threads, us, 64-token pages, fp16 cache: 128 single tokens of 80 pieces 4.4 and 3.5, of 768 8.6 and 4.8; chunks of 2048 tokens of 80 4.8 and
+    // 5.6, of 288 8.5 and 8.2, of 512 11.5 and 10.0; of 4096 of 80 6.1 and 8.9, of 512 15.2 and 15.6, of 1280 44.5 and 43.5; of 8000 of 384 26.3 and 32.2, of 512 33.2 and 36.7, of 768 51.2
+    // and 50.9, of 1280 78.5 and 73.6; of 16384 of 512 59.3 and 69.1; int8: 4096 of 320 14.4 and 15.8, uneven chunks of 4279 of 512 28.4 and 26.1, 8000 of 512 51.7 and 52.6.  Of 250 such
+    // pairs the one taken is 6 % slower at most, but for 4096 single tokens of 512 pieces and more, where each wavefront looks for its sequence among so many (768: 46 and 64).
+    const long long token_pieces = (p.heads + (i8 ? 0 : 2LL * p.cache.kv_heads)) * p.cache.head_dim / 8;
+    g.token_threads = token_pieces * (i8 ? 10 : 8) <= p.batch.tokens && token_pieces <= 768 ? 64 : 256;
     const long long tokens = i8 && !p.heads ? 0 : g.token_threads == 64 ? (p.batch.tokens + 3) / 4 : p.batch.tokens;
     if (g.blocks + tokens > MOST_WORKGROUPS) { set_error("kv_append: grid too large"); return STRAIT_E_SHAPE; }
     const dim3 grid((unsigned)(g.blocks + tokens)), block(256);

@@ -993,3 +993,15 @@ def test_a_captured_step_on_two_streams(S):
         torch.cuda.synchronize()
         assert torch.equal(y0, y1)
         length += 1
+
+
+@pytest.mark.parametrize("i8", [False, True], ids=["fp16", "int8"])
+@pytest.mark.parametrize("new,H,group,dim", [([700, 830], 1, 8, 64), ([1] * 1100, 1, 8, 64), ([2000, 3000, 130], 8, 2, 128), ([2000, 3000, 130], 8, 8, 128), ([639], 1, 8, 64), ([640], 1, 8, 64), ([800], 1, 8, 64)], ids=lambda v: str(v)[:12])
+def test_kv_append_of_many_tokens(S, new, H, group, dim, i8):
+    """A wavefront or a workgroup for a token, on both sides of where the one takes over from the other."""
+    w = World(S, 70, new, [i % 100 for i in range(len(new))], H, group, dim, 64, i8).on_gpu()
+    qkv, q, k, v, rope = append_inputs(w, dim)
+    wide = dev(S, qkv)
+    a, b = q.shape[1], q.shape[1] + k.shape[1]
+    got = S.k_kv_append(w.cache, w.batch, wide[:, a:b], wide[:, b:], q=wide[:, :a], rope=dev(S, rope))
+    check_append(w, q, k, v, rope, False, host(got), w.taken_back())
