@@ -16,20 +16,20 @@
 //     code 2^-9 of it, exactly.  The scale of the block's page multiplies the scores and the block's share of the output, in fp32;
 //   - the probabilities are the "B" operand of out^T = V^T P^T as they are, keys enumerated in the order that the scores came in; V^T's lanes
 //     read 8 keys at D / 16 dimensions each and exchange bytes within a lane.
-//   32 sequences of 1000 to 16383 tokens, 8 heads of 128 for 32, int8: 123 us, 4.6 TB/s with the join; 24 of 60000 and more, 4 heads for 32, fp16, the last 4096 and 4 of them seen: 48 us, 4.2 TB/s.
-//   One sequence of 4100: 9.7 us, the latency of two launches.
+//   32 sequences of 1000 to 16383 tokens, 8 heads of 128 for 32, int8: 118 us, 4.8 TB/s with the join; 24 of 60000 and more, 4 heads for 32, fp16, the last 4096 and 4 of them seen: 47 us, 4.3 TB/s.
+//   One sequence of 4100: 9.7 us in a graph, the latency of two launches.
 //
 //   paged_tile_kernel, 128 rows (prompts and their chunks): bound by the wavefronts' own chain of reads, products, powers and products (at two wavefronts to a SIMD, which the output's registers
-//   allow at 128 dimensions, no unit is full: vector instructions 60 % of the time, LDS 50, the matrix pipes 42).
+//   allow at 128 dimensions, no unit is full: vector instructions 62 % of the time, LDS 31, the matrix pipes 41; at 64 dimensions, three wavefronts and half the products per power, 62, 22 and 29).
 //   - 64 keys at a time go through LDS, which holds them twice as fp16: two blocks are worked on, the next two become fp16 on their way from registers to LDS, once
 //     for all four wavefronts, and the two after them are on their way from memory;
 //   - a wavefront issues in order, so its products and its vector instructions are woven by hand: the way to LDS between the products of the scores, a step's powers between
-//     the products that the step before it goes into (254 -> 243 us and 68 -> 63 us in the calls below; blocks that none
+//     the products that the step before it goes into (a twentieth of the calls below; blocks that none
 //     of a wavefront's rows see are worked on all the same, which costs nothing: the others are waited for);
 //   - scores^T with v_mfma_f32_32x32x16_f16, a row to a lane and its partner 32 lanes on; V^T's operands come from LDS transposed (ds_read_b64_tr_b16);
-//   - an int8 value's power of two is its page's, exact in fp16, and the rest of the page's scale goes into the probabilities (see look_up).
+//   - an int8 value's power of two is its page's, exact in fp16, and the rest of the page's scale goes into the powers (see look_up).
 //   Four chunks of 1200 to 2048 tokens behind up to 2048, 8 heads of 128 for 32, int8: 243 us, 755 TFLOP/s of what the masks leave; five of 333 to 4001 with a window of 1024, 12 heads
-//   of 64, fp16: 63 us, 482 TFLOP/s.
+//   of 64, fp16: 64 us, 476 TFLOP/s.
 #include <float.h>
 
 #include <algorithm>
